@@ -57,10 +57,15 @@ typedef enum {
 
 typedef enum { MT_FC = 0, MT_CONV2D = 1, MT_GAP = 2, MT_MAXPOOL = 3, MT_ADD = 4 } mt_kind;
 typedef enum { MT_ACT_NONE = 0, MT_ACT_RELU = 1, MT_ACT_GELU = 2 } mt_act;
-typedef enum { MT_F32 = 0, MT_BF16 = 1 } mt_dtype;
+typedef enum { MT_F32 = 0, MT_BF16 = 1,
+               MT_MX8 = 2        /* rows of mt_linear4 only: e4m3 values with an e8m0 scale for every MT_MX_BLOCK of a row */
+} mt_dtype;
 
 #define MT_MAX_LAYERS 48
 #define MT_SEG_SLOTS 8      /* runs made of several submissions that may be in flight at once */
+#define MT_MX_BLOCK 32      /* consecutive values of a row that share a scale in the 8-bit and 4-bit formats */
+#define MT_SCORE_MAX_TOP 32     /* most alternatives that mt_score returns for a row */
+#define MT_SCORE_MAX_GIVEN 16   /* most given classes of a row                       */
 
 /* One layer of a model (closed set, paper section 3.1; section 1.1: DNNs are built from a few
  * dozen layer types).
@@ -331,6 +336,121 @@ mt_status mt_estimate_run(mt_ctx* ctx, const uint32_t* counts, mt_run_estimate* 
 mt_status mt_admit(mt_ctx* ctx, const uint32_t* pending, double budget_ms, uint32_t* admitted, mt_run_estimate* est);
 
 mt_status mt_get_stats(const mt_ctx* ctx, mt_stats* out);
+
+/* ---- Answers of language models -------------------------------------------------------------
+ * The step behind a language model's layers, for rows of many tenants at once: mt_add_norm adds a
+ * layer's output to the residual stream and normalises it, mt_linear4 multiplies the rows of every
+ * tenant by that tenant's 4-bit weights (hidden layers, or the last one over a vocabulary), and
+ * mt_score says what the resulting logits (or those of mt_run) say about given classes.  Unlike the
+ * models of mt_run these are single operators: the caller holds every buffer between them.
+ *
+ * All pointers in the argument blocks are DEVICE memory of the context's GPU, borrowed until the work
+ * enqueued on hip_stream (a hipStream_t, NULL = default stream) has completed; the blocks themselves and
+ * group lists are HOST memory that may change as soon as the call returns.  Strides are in
+ * elements between consecutive rows (scales: in bytes, masks: in words); pointers and strides need the
+ * alignment of one element, nothing more.  The calls allocate nothing, never wait for the GPU, may be
+ * captured in a graph, and keep nothing between calls.  0 rows: MT_OK, nothing is enqueued.  Calls on different streams
+ * are independent as long as their buffers are (scratch too).
+ *
+ * 8-bit rows: values e4m3 (1 sign, 4 exponent, 3 mantissa bits, no infinities, 0x7f and 0xff NaN),
+ * and for every MT_MX_BLOCK consecutive values of a row, counted from its start, a scale e8m0 (a power of two,
+ * 2^(byte - 127); 0xff is NaN); a row's last block may be shorter.  4-bit weights: e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives, the sign is bit 3), with scales of the same kind along the fan-in. */
+
+/* h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain, row by row, in fp32, every output rounded once.
+ *   sum (h), y: in dtype; y8 with y8_scales: 8-bit rows, a block's scale the least power of two (2^-126 at least) at which none
+ *   of its values exceeds 448, 1 where all are zero; where one is infinite or NaN the block's scale and values are NaN.
+ * sum, y and y8 (with its scales) may each be NULL, not all of them; sum may be x or residual itself (same stride),
+ * y may be x or residual where sum is not; other overlaps of outputs with anything are not allowed.
+ * gain_ids[i] names row i's gain among n_gains (a tenant's); a row whose id is out of range gets y and y8 of zeros
+ * (scales 1) and touches no gain.  gain_ids NULL: every row takes the first; gain NULL: no gain is applied.
+ * Errors: MT_EINVAL (null, zero width, a stride below the width, eps negative or not finite, n_gains 0 with a gain),
+ * MT_EUNSUPPORTED (dtype other than MT_F32 and MT_BF16), MT_ESTATE (host-only context), MT_EDEVICE. */
+typedef struct {
+    const void* x;              /* [rows][x_stride], dtype                     */
+    const void* residual;       /* [rows][residual_stride], dtype, or NULL     */
+    const float* gain;          /* [n_gains][gain_stride], or NULL             */
+    const int32_t* gain_ids;    /* [rows], or NULL                             */
+    void* sum;                  /* [rows][sum_stride], dtype, or NULL          */
+    void* y;                    /* [rows][y_stride], dtype, or NULL            */
+    uint8_t* y8;                /* [rows][y8_stride], or NULL                  */
+    uint8_t* y8_scales;         /* [rows][y8_scales_stride]                    */
+    uint64_t x_stride, residual_stride, gain_stride, sum_stride, y_stride, y8_stride, y8_scales_stride;
+    uint32_t rows, width, n_gains, dtype;
+    float eps;
+    uint32_t reserved;
+} mt_norm_args;
+mt_status mt_add_norm(mt_ctx* ctx, void* hip_stream, const mt_norm_args* args);
+
+/* Bring a tenant's 4-bit matrix [out_features][in_features] into the context's arena.
+ *   codes: HOST, (in_features + 1) / 2 bytes a row, two e2m1 values to a byte, the even column in the low half;
+ *   scales: HOST e8m0, (in_features + 31) / 32 bytes a row, 27 .. 227 (2^-100 .. 2^100);
+ *   bias: HOST fp32 [out_features], or NULL for none.
+ * *matrix receives its number.  Matrices never give way to models (in a cache context models give way to them); any
+ * number of them may be registered beside the tenants' models.  The call is synchronous, like mt_register_model.
+ * mt_matrix4_footprint_get gives the bytes of arena it takes.  Errors: MT_EINVAL, MT_EUNSUPPORTED (a scale outside
+ * the range, more than 2^24 features), MT_ENOMEM, MT_EDEVICE. */
+mt_status mt_register_matrix4(mt_ctx* ctx, uint32_t out_features, uint32_t in_features, const uint8_t* codes, const uint8_t* scales,
+                              const float* bias, uint32_t* matrix);
+mt_status mt_matrix4_footprint_get(uint32_t out_features, uint32_t in_features, uint64_t* arena_bytes);
+
+/* Take a matrix out of the arena (synchronises the device first); its number may be given out again.  Errors: MT_ENOTFOUND. */
+mt_status mt_unregister_matrix4(mt_ctx* ctx, uint32_t matrix);
+
+/* y[i][n] = act(bias[n] + sum_k W[n][k] x[i][k]) for the rows i of each group, W and bias those of the group's
+ * matrix: one call serves the rows of many tenants.  Products are exact, sums fp32 (with MT_MX8 rows and an MT_BF16
+ * output: at least 2^-14 of the largest product in each 128 of the fan-in, below the output's rounding), y is rounded once.
+ * Columns of y from a matrix's out_features on, and rows in no group, are left as they are.
+ * Groups come in the order of their rows and share none; a group of 0 rows is skipped.
+ * Errors: MT_EINVAL (null, strides below a matrix's sizes, rows outside 0..rows or out of order), MT_ENOTFOUND (a
+ * matrix that is not registered), MT_EUNSUPPORTED (types, activation), MT_ESTATE (host-only context), MT_EDEVICE. */
+typedef struct { uint32_t matrix, first_row, n_rows; } mt_row_group;
+typedef struct {
+    const void* x;              /* [rows][x_stride], x_dtype                           */
+    const uint8_t* x_scales;    /* [rows][x_scales_stride], with MT_MX8; else NULL     */
+    void* y;                    /* [rows][y_stride], y_dtype; may not overlap x        */
+    uint64_t x_stride, x_scales_stride, y_stride;
+    uint32_t rows;
+    uint32_t x_dtype;           /* MT_F32, MT_BF16 or MT_MX8   */
+    uint32_t y_dtype;           /* MT_F32 or MT_BF16           */
+    uint32_t act;               /* mt_act                      */
+} mt_linear4_args;
+mt_status mt_linear4(mt_ctx* ctx, void* hip_stream, const mt_linear4_args* args, const mt_row_group* groups, uint32_t n_groups);
+
+/* What rows of logits say, with p = softmax(logits / temperature) over a row's allowed classes: those below
+ * n_classes[i] (NULL: all; the n_classes of mt_run fits) whose bit of `allowed` is set (bit c % 32 of word c / 32; NULL: all) and
+ * whose logit is not -infinity.  Everything is optional but the logits and one output:
+ *   given_logprobs[i][g] = log p of class given[i][g]; given_ranks[i][g] = allowed classes in front of it, in the order
+ *     of falling logits, lower numbers first among equals.  A class that is not allowed, or no class: -infinity and -1.
+ *   entropy[i] = -sum p log p (natural logarithm), 0 for a row without an allowed class.
+ *   top_ids[i][k], top_logprobs[i][k]: the first `top` classes in that order; past the last allowed one -1 and -infinity.
+ * A log probability beyond fp32's range is -infinity.
+ * A row with a NaN or +infinity among its allowed classes has no distribution: NaN and -1 (entries that are -infinity
+ * and -1 for want of a class stay so).  What stands in classes that are not allowed does not matter.
+ * scratch: DEVICE memory of mt_score_scratch_get's size for the call's sizes, which few rows of many classes share among
+ * workgroups; zero before its first use, left ready for the next call (of any sizes that it is large enough for), and
+ * used by one call at a time.  NULL where that size is 0.
+ * Errors: MT_EINVAL (null, no classes, a stride below the classes, temperature not positive and finite, given without
+ * classes, scratch too small, top or n_given beyond their limits), MT_EUNSUPPORTED (dtype), MT_ESTATE, MT_EDEVICE. */
+typedef struct {
+    const void* logits;             /* [rows][row_stride], dtype                        */
+    const int32_t* n_classes;       /* [rows], or NULL; taken into 0 .. classes         */
+    const uint32_t* allowed;        /* [rows][allowed_stride], or NULL                  */
+    const int32_t* given;           /* [rows][n_given], or NULL with n_given 0          */
+    float* given_logprobs;          /* [rows][n_given], or NULL                         */
+    int32_t* given_ranks;           /* [rows][n_given], or NULL                         */
+    float* entropy;                 /* [rows], or NULL                                  */
+    int32_t* top_ids;               /* [rows][top], or NULL                             */
+    float* top_logprobs;            /* [rows][top], or NULL                             */
+    void* scratch;
+    uint64_t scratch_bytes;
+    uint64_t row_stride, allowed_stride;
+    uint32_t rows, classes, n_given, top;
+    uint32_t dtype;                 /* MT_F32 or MT_BF16                                */
+    float temperature;
+} mt_score_args;
+mt_status mt_score(mt_ctx* ctx, void* hip_stream, const mt_score_args* args);
+mt_status mt_score_scratch_get(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top, uint64_t* bytes);
 
 /* Text of the last error on this context ("" if none); valid until the next call. */
 const char* mt_last_error(const mt_ctx* ctx);

@@ -21,8 +21,10 @@ STATUS_NAMES = {0: "MT_OK", 1: "MT_EINVAL", 2: "MT_ENOMEM", 3: "MT_ENOTFOUND", 4
                 5: "MT_EUNSUPPORTED", 6: "MT_EFULL", 7: "MT_ESTATE", 8: "MT_EDEVICE"}
 MT_FC, MT_CONV2D, MT_GAP, MT_MAXPOOL, MT_ADD = 0, 1, 2, 3, 4
 MT_ACT_NONE, MT_ACT_RELU, MT_ACT_GELU = 0, 1, 2
-MT_F32, MT_BF16 = 0, 1
+MT_F32, MT_BF16, MT_MX8 = 0, 1, 2
 MT_MAX_LAYERS = 48
+MT_MX_BLOCK = 32
+MT_SCORE_MAX_TOP, MT_SCORE_MAX_GIVEN = 32, 16
 
 
 class MtError(RuntimeError):
@@ -73,6 +75,28 @@ class mt_outputs(ctypes.Structure):
 class mt_stats(ctypes.Structure):
     _fields_ = [("n_tenants", ctypes.c_uint32), ("arena_used", ctypes.c_uint64), ("arena_bytes", ctypes.c_uint64),
                 ("last_run_rows", ctypes.c_uint32), ("last_run_launches", ctypes.c_uint32)]
+
+
+class mt_norm_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "residual", "gain", "gain_ids", "sum", "y", "y8", "y8_scales")] +
+                [(n, ctypes.c_uint64) for n in ("x_stride", "residual_stride", "gain_stride", "sum_stride", "y_stride", "y8_stride", "y8_scales_stride")] +
+                [(n, ctypes.c_uint32) for n in ("rows", "width", "n_gains", "dtype")] + [("eps", ctypes.c_float), ("reserved", ctypes.c_uint32)])
+
+
+class mt_row_group(ctypes.Structure):
+    _fields_ = [("matrix", ctypes.c_uint32), ("first_row", ctypes.c_uint32), ("n_rows", ctypes.c_uint32)]
+
+
+class mt_linear4_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "x_scales", "y")] + [(n, ctypes.c_uint64) for n in ("x_stride", "x_scales_stride", "y_stride")] +
+                [(n, ctypes.c_uint32) for n in ("rows", "x_dtype", "y_dtype", "act")])
+
+
+class mt_score_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("logits", "n_classes", "allowed", "given", "given_logprobs", "given_ranks", "entropy", "top_ids",
+                                                "top_logprobs", "scratch")] +
+                [(n, ctypes.c_uint64) for n in ("scratch_bytes", "row_stride", "allowed_stride")] +
+                [(n, ctypes.c_uint32) for n in ("rows", "classes", "n_given", "top", "dtype")] + [("temperature", ctypes.c_float)])
 
 
 class mt_profile(ctypes.Structure):
@@ -126,13 +150,21 @@ def load_library() -> ctypes.CDLL:
     L.mt_debug_conv_launch.argtypes = [vp, u32, u32, ctypes.POINTER(u32), ctypes.POINTER(u32), ctypes.POINTER(ctypes.c_uint64)]
     L.mt_set_profiling.argtypes = [vp, ctypes.c_int]
     L.mt_get_profile.argtypes = [vp, ctypes.POINTER(mt_profile)]
+    L.mt_add_norm.argtypes = [vp, vp, ctypes.POINTER(mt_norm_args)]
+    L.mt_register_matrix4.argtypes = [vp, u32, u32, vp, vp, vp, ctypes.POINTER(u32)]
+    L.mt_matrix4_footprint_get.argtypes = [u32, u32, ctypes.POINTER(ctypes.c_uint64)]
+    L.mt_unregister_matrix4.argtypes = [vp, u32]
+    L.mt_linear4.argtypes = [vp, vp, ctypes.POINTER(mt_linear4_args), ctypes.POINTER(mt_row_group), u32]
+    L.mt_score.argtypes = [vp, vp, ctypes.POINTER(mt_score_args)]
+    L.mt_score_scratch_get.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_uint64)]
     L.mt_last_error.argtypes = [vp]
     L.mt_last_error.restype = ctypes.c_char_p
     L.mt_version.restype = ctypes.c_char_p
     for name in ("mt_create", "mt_destroy", "mt_register_model", "mt_register_model_bn", "mt_unregister_model", "mt_submit",
                  "mt_submit_batch", "mt_run", "mt_run_static", "mt_last_counts", "mt_get_stats", "mt_tenant_account_get", "mt_estimate_run", "mt_prefetch", "mt_cache_stats_get", "mt_admit", "mt_debug_poison", "mt_debug_copy",
                  "mt_set_profiling", "mt_get_profile", "mt_model_footprint_get", "mt_debug_mfma_rate",
-                 "mt_debug_conv_launch"):
+                 "mt_debug_conv_launch", "mt_add_norm", "mt_register_matrix4", "mt_matrix4_footprint_get", "mt_unregister_matrix4", "mt_linear4",
+                 "mt_score", "mt_score_scratch_get"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -296,6 +328,33 @@ class Context:
         self._check(self._lib.mt_cache_stats_get(self._h, ctypes.byref(st)))
         return {k: int(getattr(st, k)) for k, _ in mt_cache_stats._fields_}
 
+    # -- operators behind language models' answers ---------------------------------------------
+    def register_matrix4(self, out_features: int, in_features: int, codes, scales, bias=None) -> int:
+        """mt_register_matrix4: host arrays codes [out][(in + 1) / 2] and scales [out][(in + 31) / 32] of bytes, bias fp32 [out] or None."""
+        c, e = (np.ascontiguousarray(v, dtype=np.uint8) for v in (codes, scales))
+        if c.shape != (out_features, (in_features + 1) // 2) or e.shape != (out_features, -(-in_features // MT_MX_BLOCK)):
+            raise ValueError("codes %s and scales %s do not fit %d x %d weights" % (c.shape, e.shape, out_features, in_features))
+        b = None if bias is None else np.ascontiguousarray(bias, dtype=np.float32)
+        if b is not None and b.shape != (out_features,):
+            raise ValueError("a bias of shape %s for %d outputs" % (b.shape, out_features))
+        number = ctypes.c_uint32(0)
+        self._check(self._lib.mt_register_matrix4(self._h, out_features, in_features, c.ctypes.data, e.ctypes.data, b.ctypes.data if b is not None else None,
+                                                  ctypes.byref(number)))
+        return number.value
+
+    def unregister_matrix4(self, matrix: int):
+        self._check(self._lib.mt_unregister_matrix4(self._h, matrix))
+
+    def add_norm(self, stream_ptr: int, args: mt_norm_args):
+        self._check(self._lib.mt_add_norm(self._h, stream_ptr or None, ctypes.byref(args)))
+
+    def linear4(self, stream_ptr: int, args: mt_linear4_args, groups):
+        """`groups`: a ctypes array of mt_row_group (row_groups)."""
+        self._check(self._lib.mt_linear4(self._h, stream_ptr or None, ctypes.byref(args), groups, len(groups)))
+
+    def score(self, stream_ptr: int, args: mt_score_args):
+        self._check(self._lib.mt_score(self._h, stream_ptr or None, ctypes.byref(args)))
+
     def stats(self) -> dict:
         s = mt_stats()
         self._check(self._lib.mt_get_stats(self._h, ctypes.byref(s)))
@@ -310,6 +369,30 @@ def model_footprint(specs: Sequence[mt_layer_spec], dtype: int) -> dict:
     if st != MT_OK:
         raise MtError(st, "mt_model_footprint_get failed")
     return {"arena_bytes": int(f.arena_bytes), "min_width": int(f.min_width), "n_classes": int(f.n_classes), "in_len": int(f.in_len)}
+
+
+def matrix4_footprint(out_features: int, in_features: int) -> int:
+    """mt_matrix4_footprint_get: bytes of arena that a 4-bit matrix takes."""
+    n = ctypes.c_uint64()
+    st = load_library().mt_matrix4_footprint_get(out_features, in_features, ctypes.byref(n))
+    if st != MT_OK:
+        raise MtError(st, "no matrix has %d x %d features" % (out_features, in_features))
+    return int(n.value)
+
+
+def row_groups(groups):
+    """(matrix, first row, rows) of every group, as mt_linear4 takes them."""
+    g = list(groups)
+    return (mt_row_group * len(g))(*[mt_row_group(*(int(v) for v in t)) for t in g])
+
+
+def score_scratch(rows: int, classes: int, n_given: int, top: int) -> int:
+    """mt_score_scratch_get: bytes of scratch that a call of these sizes needs."""
+    n = ctypes.c_uint64()
+    st = load_library().mt_score_scratch_get(rows, classes, n_given, top, ctypes.byref(n))
+    if st != MT_OK:
+        raise MtError(st, "%d classes, %d given, %d alternatives" % (classes, n_given, top))
+    return int(n.value)
 
 
 def debug_mfma_rate(stream: int = 0) -> float:

@@ -1,0 +1,69 @@
+// Device helpers shared by the operators behind language models' answers (lm_*.hip).
+#pragma once
+#include "mt_device.h"
+
+namespace mt {
+
+// Loads and stores of 16 or 8 bytes at any element's address.
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <typename T> struct Any;
+template <> struct Any<uint8_t> { typedef u32x4 vec16 __attribute__((aligned(1))); typedef u32x2 vec8 __attribute__((aligned(1))); };
+template <> struct Any<__bf16> { typedef u32x4 vec16 __attribute__((aligned(2))); typedef u32x2 vec8 __attribute__((aligned(2))); };
+template <> struct Any<float> { typedef u32x4 vec16 __attribute__((aligned(4))); typedef u32x2 vec8 __attribute__((aligned(4))); };
+
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }
+// two fp32 to bf16 (nearest even), packed
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)lo, (__bf16)hi});
+}
+
+// Eight consecutive elements as fp32, from any element's address.
+__device__ __forceinline__ void load8(const __bf16* p, float (&v)[8])
+{
+    const u32x4 w = *(const Any<__bf16>::vec16*)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(w[i]); v[2 * i + 1] = bf16_hi(w[i]); }
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8])
+{
+    // (whole vectors: the compiler takes element 0 for every element of one that is cast by elements)
+    const f32x4 a = __builtin_bit_cast(f32x4, *(const Any<float>::vec16*)p), b = __builtin_bit_cast(f32x4, *(const Any<float>::vec16*)(p + 4));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+}
+__device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    *(Any<__bf16>::vec16*)p = w;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8])
+{
+    const f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
+    *(Any<float>::vec16*)p = __builtin_bit_cast(u32x4, a); *(Any<float>::vec16*)(p + 4) = __builtin_bit_cast(u32x4, b);
+}
+// The first n (0 .. 8) of them, element by element; zeros behind.
+template <typename T> __device__ __forceinline__ void load_some(const T* p, uint32_t n, float (&v)[8])
+{
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+}
+template <typename T> __device__ __forceinline__ void store_some(T* p, uint32_t n, const float (&v)[8])
+{
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) if (i < n) p[i] = (T)v[i];
+}
+
+// Sum over the wave, in every lane.
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+}  // namespace mt

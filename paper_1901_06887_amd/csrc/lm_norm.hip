@@ -1,0 +1,183 @@
+// mt_add_norm: residual addition, root-mean-square norm and the 8-bit rows, one pass over memory.
+//
+// h = x + r, y = h * rsqrt(mean(h^2) + eps) * gain, q = e4m3(y / 2^e) with the least e >= -126 for which no |y| of the
+// 32 values exceeds 448 * 2^e.  A row is read once and stays in registers between the sum of squares and the outputs; a lane
+// holds runs of eight consecutive elements, so a block of 32 is four neighbouring lanes and its maximum two cross-lane moves.
+#include "lm_device.h"
+
+namespace mt {
+namespace {
+
+constexpr uint32_t kRun = 8;                  // consecutive elements of a lane
+
+// 2^e for -126 <= e <= 127
+__device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
+
+// e for a block whose largest magnitude is `most` (not NaN, not infinite): 448 is 1.75 * 2^8
+__device__ __forceinline__ int block_exponent(float most)
+{
+    const uint32_t b = __builtin_bit_cast(uint32_t, most);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return most > 0.0f ? max(e, -126) : 0;
+}
+
+template <typename T>
+struct NormRow {
+    const T* x; const T* residual; const float* gain;
+    T* sum; T* y; uint8_t* y8; uint8_t* y8_scales;
+    bool known;                               // the row's gain exists
+};
+
+template <typename T>
+__device__ __forceinline__ NormRow<T> norm_row(const mt_norm_args& a, uint32_t row)
+{
+    NormRow<T> r;
+    r.x = (const T*)a.x + row * a.x_stride;
+    r.residual = a.residual ? (const T*)a.residual + row * a.residual_stride : nullptr;
+    r.known = true;
+    uint32_t id = 0;
+    if (a.gain_ids) { id = (uint32_t)a.gain_ids[row]; r.known = id < a.n_gains; }
+    r.gain = a.gain && r.known ? a.gain + id * a.gain_stride : nullptr;
+    r.sum = a.sum ? (T*)a.sum + row * a.sum_stride : nullptr;
+    r.y = a.y ? (T*)a.y + row * a.y_stride : nullptr;
+    r.y8 = a.y8 ? a.y8 + row * a.y8_stride : nullptr;
+    r.y8_scales = a.y8_scales ? a.y8_scales + row * a.y8_scales_stride : nullptr;
+    return r;
+}
+
+// A lane's run of the row at `at`: h in fp32, zeros past the width.
+template <typename T>
+__device__ __forceinline__ void load_run(const NormRow<T>& r, uint32_t at, uint32_t width, float (&h)[kRun])
+{
+    if (at + kRun <= width) {
+        load8(r.x + at, h);
+        if (r.residual) {
+            float q[kRun];
+            load8(r.residual + at, q);
+#pragma unroll
+            for (uint32_t i = 0; i < kRun; ++i) h[i] += q[i];
+        }
+        return;
+    }
+    const uint32_t n = at < width ? width - at : 0;
+    load_some(r.x + at, n, h);
+    if (r.residual) {
+        float q[kRun];
+        load_some(r.residual + at, n, q);
+#pragma unroll
+        for (uint32_t i = 0; i < kRun; ++i) h[i] += q[i];
+    }
+}
+
+// Everything behind the mean: the run's sum, norm and 8-bit values.  All lanes of a block come here together.
+template <typename T>
+__device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uint32_t width, const float (&h)[kRun], float scale)
+{
+    const uint32_t n = at >= width ? 0 : width - at < kRun ? width - at : kRun;
+    float y[kRun], g[kRun];
+    if (r.gain) {
+        if (n == kRun) load8(r.gain + at, g); else load_some(r.gain + at, n, g);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < kRun; ++i) {
+        y[i] = h[i] * scale;
+        if (r.gain) y[i] *= g[i];
+        if (!r.known || i >= n) y[i] = 0.0f;
+    }
+    if (r.sum && n) { if (n == kRun) store8(r.sum + at, h); else store_some(r.sum + at, n, h); }
+    if (r.y && n) { if (n == kRun) store8(r.y + at, y); else store_some(r.y + at, n, y); }
+    if (!r.y8) return;
+    // magnitudes as integers: they order like the values, and a NaN stays above every number
+    uint32_t most = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kRun; ++i) most = max(most, __builtin_bit_cast(uint32_t, y[i]) & 0x7fffffffu);
+    most = max(most, (uint32_t)__shfl_xor((int)most, 1));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 2));
+    const bool finite = most < 0x7f800000u;
+    const int e = finite ? block_exponent(__builtin_bit_cast(float, most)) : 0;
+    const float down = power(-e);             // e is at most 119 + 1
+    uint32_t q[2];
+#pragma unroll
+    for (uint32_t i = 0; i < 2; ++i) {
+        int w = 0;
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i] * down, y[4 * i + 1] * down, w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * down, y[4 * i + 3] * down, w, true);
+        q[i] = finite ? (uint32_t)w : 0x7f7f7f7fu;
+    }
+    if (n == kRun) *(Any<uint8_t>::vec8*)(r.y8 + at) = Any<uint8_t>::vec8{q[0], q[1]};
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < kRun; ++i) if (i < n) r.y8[at + i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
+    if (n && at % MT_MX_BLOCK == 0) r.y8_scales[at / MT_MX_BLOCK] = finite ? (uint8_t)(e + 127) : 0xff;
+}
+
+// THREADS to a row, each with RUNS runs of it in registers (run j of thread t at (j * THREADS + t) * 8); WGS rows to a workgroup
+// of one wave each where THREADS is 64.  LOOP: a row that no workgroup holds is read a second time for the outputs.
+template <typename T, uint32_t THREADS, uint32_t RUNS, bool LOOP>
+__global__ void __launch_bounds__(THREADS == 64 ? 256 : THREADS) norm_kernel(mt_norm_args a)
+{
+    constexpr uint32_t kSpan = THREADS * kRun;
+    const uint32_t t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
+    const uint32_t row = THREADS == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
+    if (row >= a.rows) return;                // (whole waves, and only where no barrier follows)
+    const NormRow<T> r = norm_row<T>(a, row);
+    float h[RUNS][kRun];
+    float squares = 0.0f;
+    for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * kSpan) {
+#pragma unroll
+        for (uint32_t j = 0; j < RUNS; ++j) {
+            load_run(r, base + j * kSpan + t * kRun, a.width, h[j]);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < RUNS; ++j)
+#pragma unroll
+            for (uint32_t i = 0; i < kRun; ++i) squares = fmaf(h[j][i], h[j][i], squares);
+    }
+    squares = wave_sum(squares);
+    if constexpr (THREADS > 64) {
+        __shared__ float part[THREADS / 64];
+        if ((t & 63) == 0) part[t >> 6] = squares;
+        __syncthreads();
+        squares = 0.0f;
+#pragma unroll
+        for (uint32_t w = 0; w < THREADS / 64; ++w) squares += part[w];
+    }
+    const float scale = 1.0f / __builtin_sqrtf(squares / (float)a.width + a.eps);
+    for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * kSpan) {
+#pragma unroll
+        for (uint32_t j = 0; j < RUNS; ++j) {
+            const uint32_t at = base + j * kSpan + t * kRun;
+            if (LOOP) load_run(r, at, a.width, h[j]);
+            finish_run(r, at, a.width, h[j], scale);
+        }
+    }
+}
+
+template <typename T, uint32_t THREADS, uint32_t RUNS, bool LOOP = false>
+hipError_t go(const mt_norm_args& a, hipStream_t s)
+{
+    const uint32_t grid = THREADS == 64 ? (a.rows + 3) / 4 : a.rows;
+    hipLaunchKernelGGL((norm_kernel<T, THREADS, RUNS, LOOP>), dim3(grid), dim3(THREADS == 64 ? 256 : THREADS), 0, s, a);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t choose(const mt_norm_args& a, hipStream_t s)
+{
+    if (a.width <= 512) return go<T, 64, 1>(a, s);
+    if (a.width <= 1024) return go<T, 64, 2>(a, s);
+    if (a.width <= 2048) return go<T, 256, 1>(a, s);
+    if (a.width <= 4096) return go<T, 256, 2>(a, s);
+    if (a.width <= 8192) return go<T, 256, 4>(a, s);
+    if (a.width <= 16384) return go<T, 1024, 2>(a, s);
+    return go<T, 1024, 2, true>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_norm(const mt_norm_args& a, hipStream_t s)
+{
+    return a.dtype == MT_BF16 ? choose<__bf16>(a, s) : choose<float>(a, s);
+}
+
+}  // namespace mt

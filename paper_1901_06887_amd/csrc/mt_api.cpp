@@ -242,6 +242,8 @@ struct mt_ctx {
     std::vector<PlanUse> plans_used;        // by those captured before, oldest first, each kind once (the newest of it); at most kPlansKept
     uint32_t plans_dropped = 0;             // the newest of those no longer known
 
+    std::vector<Matrix4> matrices;          // 4-bit matrices by number (lm_api.cpp)
+
     // pending submissions
     std::vector<Segment> pending;
     uint32_t pending_rows = 0;
@@ -1320,6 +1322,34 @@ uint64_t layout_model(HostTenant* ht)
 }
 
 }  // namespace
+
+namespace mt {
+
+CtxView ctx_view(mt_ctx* c) { return CtxView{c->host_only, c->cfg.device, c->n_cus, c->d_arena, &c->matrices}; }
+
+mt_status ctx_fail(mt_ctx* c, mt_status st, const char* fmt, ...)
+{
+    char buf[512];
+    va_list ap; va_start(ap, fmt); vsnprintf(buf, sizeof buf, fmt, ap); va_end(ap);
+    return fail(c, st, "%s", buf);
+}
+
+mt_status ctx_arena_take(mt_ctx* c, uint64_t len, uint64_t* off)
+{
+    if (len > c->cfg.arena_bytes)
+        return fail(c, MT_ENOMEM, "matrix needs %llu bytes, the weight arena has %llu", (unsigned long long)len, (unsigned long long)c->cfg.arena_bytes);
+    // as for models: nothing that a run in flight reads may give way, and a block freed by an earlier eviction may still be read
+    if (c->cache && !c->host_only) HIP_TRY(c, hipDeviceSynchronize());
+    hipError_t e = hipSuccess;
+    if (make_room(c, len, ++c->use_clock, nullptr, false, off, &e)) return MT_OK;
+    if (e != hipSuccess) return fail(c, MT_EDEVICE, "eviction failed: %s", hipGetErrorString(e));
+    return fail(c, MT_ENOMEM, "weight arena exhausted: matrix needs %llu bytes, %llu of %llu in use",
+                (unsigned long long)len, (unsigned long long)c->arena_used, (unsigned long long)c->cfg.arena_bytes);
+}
+
+void ctx_arena_give(mt_ctx* c, uint64_t off, uint64_t len) { arena_free(c, off, len); }
+
+}  // namespace mt
 
 extern "C" {
 
