@@ -1,13 +1,33 @@
-// mt_score: log probabilities and ranks of given classes, entropy and the best alternatives of rows of logits.
+// mt_score: log probabilities and ranks of given classes, entropy and the best alternatives of rows of logits, in one pass over them.
 //
 // With m the largest allowed logit, z = (x - m) / T, S = sum e^z and U = sum z e^z: log p = z - log S and the entropy is log S - U / S, a sum of two
-// terms that are not negative.  (x - m) / 2 is what is worked with: x - m itself can leave fp32's range.
+// terms that are not negative.  (x - m) / 2 is what is worked with: x - m itself can leave fp32's range.  Every lane carries its own m, S and U and
+// rescales them once per 16 classes; lanes, waves and workgroups are joined at the end.
+//
+// Alternatives: every wave keeps a list in LDS of what can still be among the best `top` of its classes.  Its first 1024 classes set a bar: the
+// top-th largest of the lanes' maxima, which at least `top` of them reach and few others do.  Later classes are in lane order behind those, so an equal
+// one never gets in; a list that fills up is cut to its best `top` and raises the bar.  One comparison a lane and 16 classes is what that costs where nothing passes.
 #include "lm_device.h"
 
 namespace mt {
 namespace {
 
 constexpr float kNone = -__builtin_inff();
+constexpr float kLowest = -3.402823466e38f;
+constexpr uint32_t kPer = 16;                     // classes of a lane at a time
+constexpr uint32_t kChunk = 64 * kPer;            // ... of a wave
+constexpr uint32_t kList = 192;                   // entries of a wave's list
+constexpr uint32_t kWaves = 4;                    // waves of a workgroup
+constexpr uint32_t kSplitRows = 1024;             // most rows whose classes workgroups share
+constexpr uint32_t kMaxParts = 64;                // most workgroups that share one
+constexpr uint32_t kPartKeys = kMaxParts / kWaves * MT_SCORE_MAX_TOP / 64;      // keys of a lane where parts are joined
+
+// What a workgroup hands over of its share of a row.
+struct Part {
+    float m, s, u; uint32_t pad;
+    uint32_t in_front[MT_SCORE_MAX_GIVEN];
+    uint64_t keys[MT_SCORE_MAX_TOP];
+};
 
 // A class's logit, -infinity where it is not allowed.
 template <typename T>
@@ -17,106 +37,425 @@ __device__ __forceinline__ float logit(const T* x, const uint32_t* allowed, uint
     return (float)x[c];
 }
 
-// Order of classes: larger logit first, then lower number; as one integer, larger in front.  0: no class.
+// Order of classes: larger logit first, then lower number; as one integer, larger in front.  0 is no class.
 __device__ __forceinline__ uint64_t order_key(float x, uint32_t c)
 {
-    if (x == kNone) return 0;
     uint32_t b = __builtin_bit_cast(uint32_t, x == 0.0f ? 0.0f : x);      // (both zeros are equal)
     b = b & 0x80000000u ? ~b : b | 0x80000000u;
     return (uint64_t)b << 32 | (0xffffffffu - c);
 }
+__device__ __forceinline__ float key_logit(uint64_t key)
+{
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __builtin_bit_cast(float, b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+__device__ __forceinline__ int32_t key_class(uint64_t key) { return (int32_t)(0xffffffffu - (uint32_t)key); }
 
 // Half of x - m: with finite x and m this is never out of range.
 __device__ __forceinline__ float half_below(float x, float m) { return fmaf(0.5f, x, -0.5f * m); }
 __device__ __forceinline__ float log_prob(float x, float m, float inv_t, float log_s) { return half_below(x, m) * inv_t * 2.0f - log_s; }
 
-template <typename V, typename F>
-__device__ __forceinline__ V over_workgroup(V v, V* lds, F f)
+// Maximum and sums of some classes; nothing yet: {kLowest, 0, 0}.
+struct Sums {
+    float m, s, u;
+    __device__ __forceinline__ void rebase(float to, float scale)
+    {
+        const float d = half_below(m, to), f = __builtin_amdgcn_exp2f(d * scale);
+        u = f * fmaf(fmaxf(d, -1e30f), s, u);
+        s *= f;
+        m = to;
+    }
+    __device__ __forceinline__ void join(const Sums& o, float scale)
+    {
+        const float to = fmaxf(m, o.m);
+        Sums q = o;
+        q.rebase(to, scale);
+        rebase(to, scale);
+        s += q.s; u += q.u;
+    }
+    __device__ __forceinline__ void over_wave(float scale)
+    {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) join(Sums{__shfl_xor(m, d), __shfl_xor(s, d), __shfl_xor(u, d)}, scale);
+    }
+};
+
+// Between writes and reads of LDS by lanes of one wave.
+__device__ __forceinline__ void wave_sync()
 {
-    for (int d = 1; d < 64; d *= 2) v = f(v, __shfl_xor(v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (uint32_t w = 1; w < blockDim.x / 64; ++w) v = f(v, lds[w]);
-    return v;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+    __builtin_amdgcn_wave_barrier();
 }
 
-// One workgroup to a row: its maximum, its sums, ranks, and the alternatives one after the other.
-template <typename T>
+// Entries of a wave's list, and the bar: a class is kept if its logit is above `bar`, or equal to `equal` (NaN: to nothing).
+struct List {
+    uint64_t* at;         // LDS, kList entries
+    uint32_t n;
+    float bar, equal;
+    __device__ __forceinline__ bool keeps(float x) const { return x > bar || x == equal; }
+
+    // The best `top` of the entries, in order; raises the bar to the last of them.
+    __device__ __forceinline__ void cut(uint32_t top, uint32_t lane)
+    {
+        if (lane < 4) at[n + lane] = 0;           // (the loop below takes four at a time; the list has room for them)
+        wave_sync();
+        uint64_t own[kList / 64];
+        uint32_t before[kList / 64];
+#pragma unroll
+        for (uint32_t j = 0; j < kList / 64; ++j) { own[j] = 64 * j + lane < n ? at[64 * j + lane] : 0; before[j] = own[j] ? 0 : kList; }
+        if (n <= 64) {
+            for (uint32_t i = 0; i < n; i += 4)
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) before[0] += at[i + k] > own[0];
+        } else {
+            for (uint32_t i = 0; i < n; i += 4)
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const uint64_t e = at[i + k];
+#pragma unroll
+                    for (uint32_t j = 0; j < kList / 64; ++j) before[j] += e > own[j];
+                }
+        }
+        wave_sync();
+#pragma unroll
+        for (uint32_t j = 0; j < kList / 64; ++j) if (before[j] < top) at[before[j]] = own[j];
+        wave_sync();
+        if (n >= top) {
+            n = top;
+            equal = bar = key_logit(at[top - 1]);
+        }
+    }
+
+    __device__ __forceinline__ void append(bool keep, uint64_t key)
+    {
+        const uint64_t lanes = __ballot(keep);
+        if (keep) at[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0))] = key;
+        n += (uint32_t)__popcll(lanes);
+    }
+};
+constexpr uint32_t kListRoom = kList - 64 - 4;    // entries after which every lane can still append one
+
+// The top-th largest of the lanes' values, rounded down a little; -infinity if there are not so many.
+__device__ __forceinline__ float bar_of(float v, uint32_t top)
+{
+    // by bits from the highest, over values ordered as integers; 20 of them decide
+    uint32_t b = __builtin_bit_cast(uint32_t, v);
+    b = v == kNone ? 0 : b & 0x80000000u ? ~b : b | 0x80000000u;
+    uint32_t found = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 12; --bit) {
+        const uint32_t probe = found | 1u << bit;
+        if ((uint32_t)__popcll(__ballot(b >= probe)) >= top) found = probe;
+    }
+    if (found == 0) return kNone;
+    const float bar = __builtin_bit_cast(float, found & 0x80000000u ? found ^ 0x80000000u : ~found);
+    return bar == bar ? bar : kNone;              // (bits of a NaN below all numbers: not so many of them)
+}
+
+// A lane's 16 classes of a chunk as they come from memory: vectors of 16 bytes, 64 of them side by side.
+template <typename T> struct Raw {
+    static constexpr uint32_t kVec = 16 / sizeof(T), kVecs = kPer / kVec;
+    u32x4 v[kVecs];
+    uint32_t bits[kVecs];
+
+    static __device__ __forceinline__ uint32_t first(uint32_t base, uint32_t i, uint32_t lane) { return base + (i * 64 + lane) * kVec; }
+
+    template <bool MASK>
+    __device__ __forceinline__ void load(const T* x, const uint32_t* allowed, uint32_t base, uint32_t lane, uint32_t classes)
+    {
+        if (base + kChunk <= classes) {
+#pragma unroll
+            for (uint32_t i = 0; i < kVecs; ++i) v[i] = *(const typename Any<T>::vec16*)(x + first(base, i, lane));
+        } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kVecs; ++i) {
+                const uint32_t c = first(base, i, lane);
+                v[i] = u32x4{0, 0, 0, 0};
+                if (c + kVec <= classes) v[i] = *(const typename Any<T>::vec16*)(x + c);
+                else if (c < classes) {
+#pragma unroll
+                    for (uint32_t e = 0; e < kVec; ++e)
+                        if (c + e < classes) {
+                            if constexpr (sizeof(T) == 2) v[i][e / 2] |= (uint32_t)((const uint16_t*)x)[c + e] << (16 * (e % 2));
+                            else v[i][e] = ((const uint32_t*)x)[c + e];
+                        }
+                }
+            }
+        }
+        if constexpr (MASK) {
+#pragma unroll
+            for (uint32_t i = 0; i < kVecs; ++i) {
+                const uint32_t c = first(base, i, lane);
+                bits[i] = c < classes ? allowed[c >> 5] >> (c & 31) : 0;
+            }
+        }
+    }
+
+    template <bool MASK>
+    __device__ __forceinline__ void logits(float (&x)[kPer], uint32_t base, uint32_t lane, uint32_t n) const
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs; ++i) {
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) { x[8 * i + 2 * e] = bf16_lo(v[i][e]); x[8 * i + 2 * e + 1] = bf16_hi(v[i][e]); }
+            } else {
+                const f32x4 f = __builtin_bit_cast(f32x4, v[i]);
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e) x[4 * i + e] = f[e];
+            }
+            if constexpr (MASK) {
+#pragma unroll
+                for (uint32_t e = 0; e < kVec; ++e) if (!((bits[i] >> e) & 1)) x[kVec * i + e] = kNone;
+            }
+        }
+        if (base + kChunk > n) {
+#pragma unroll
+            for (uint32_t i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (uint32_t e = 0; e < kVec; ++e) if (first(base, i, lane) + e >= n) x[kVec * i + e] = kNone;
+        }
+    }
+};
+
+// Everything that a wave, then a workgroup, knows of its share of a row.
+struct Share {
+    Sums sums;
+    uint32_t in_front;        // lane g: allowed classes in front of given class g
+};
+
+// WAVES waves share a row's part [blockIdx.y]; WAVES 1: every wave of the workgroup has a row of its own.
+template <typename T, bool TOP, bool MASK, uint32_t WAVES>
 __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
 {
-    __shared__ float fl[4];
-    __shared__ uint64_t kl[4];
     const mt_score_args& a = s.a;
-    const uint64_t row = blockIdx.x;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t row = WAVES == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
+    if (row >= a.rows) return;                    // (whole waves, and none where a barrier follows)
+    __shared__ __attribute__((aligned(16))) uint64_t lists[TOP ? kWaves : 1][TOP ? kList : 1];
     const T* x = (const T*)a.logits + row * a.row_stride;
-    const uint32_t* allowed = a.allowed ? a.allowed + row * a.allowed_stride : nullptr;
+    const uint32_t* allowed = MASK ? a.allowed + row * a.allowed_stride : nullptr;
+    const uint32_t part = WAVES == 1 ? 0 : blockIdx.y;
+    const uint32_t part_end = min((uint64_t)(part + 1) * s.part_len, (uint64_t)a.classes);
+    const uint32_t wave_len = WAVES == 1 ? s.part_len : (s.part_len / WAVES + kChunk - 1) / kChunk * kChunk;
+    uint32_t base = part * s.part_len + (WAVES == 1 ? 0 : wave * wave_len);
+    const uint32_t mem_end = base < part_end ? min((uint64_t)base + wave_len, (uint64_t)part_end) : base;      // this wave's classes, and no more are read
+    Raw<T> raw;
+    if (base < mem_end) raw.template load<MASK>(x, allowed, base, lane, mem_end);
     const uint32_t n = a.n_classes ? (uint32_t)min(max(a.n_classes[row], 0), (int32_t)a.classes) : a.classes;
-    const auto larger = [](float p, float q) { return fmaxf(p, q); };
-    const auto sum = [](float p, float q) { return p + q; };
-    float m = kNone;
-    uint32_t count = 0;
-    for (uint32_t c = threadIdx.x; c < n; c += 256) { const float v = logit(x, allowed, c, n); m = fmaxf(m, v); count |= v != kNone; }
-    m = over_workgroup(m, fl, larger);
-    const bool some = over_workgroup(count, (uint32_t*)fl, [](uint32_t p, uint32_t q) { return p | q; }) != 0;      // (a NaN is no maximum)
-    float S = 0.0f, U = 0.0f;
-    if (some)
-        for (uint32_t c = threadIdx.x; c < n; c += 256) {
-            const float h = half_below(logit(x, allowed, c, n), m);
+    const uint32_t end = min(mem_end, n);
+    // lane g: given class g and its logit
+    const int32_t given = lane < a.n_given ? a.given[(uint64_t)row * a.n_given + lane] : -1;
+    const float given_x = given >= 0 ? logit(x, allowed, (uint32_t)given, n) : kNone;
+
+    Share w{{kLowest, 0.0f, 0.0f}, 0};
+    List list{TOP ? lists[wave] : nullptr, 0, kNone, __builtin_nanf("")};
+    for (; base < end; base += kChunk) {
+        float v[kPer];
+        raw.template logits<MASK>(v, base, lane, end);
+        if (base + kChunk < end) raw.template load<MASK>(x, allowed, base + kChunk, lane, mem_end);
+        float most = v[0];
+#pragma unroll
+        for (uint32_t i = 1; i < kPer; ++i) most = fmaxf(most, v[i]);
+        w.sums.rebase(fmaxf(w.sums.m, most), s.exp2_scale);
+#pragma unroll
+        for (uint32_t i = 0; i < kPer; ++i) {
+            const float h = half_below(v[i], w.sums.m);
             const float e = __builtin_amdgcn_exp2f(h * s.exp2_scale);
-            S += e; U = fmaf(fmaxf(h, -1e30f), e, U);
+            w.sums.s += e;
+            w.sums.u = fmaf(fmaxf(h, -1e30f), e, w.sums.u);
         }
-    S = over_workgroup(S, fl, sum);
-    U = over_workgroup(U, fl, sum);
-    const bool lost = some && !(S < __builtin_inff());         // NaN or +infinity among the allowed
-    const float log_s = logf(S);
-    const float nan = __builtin_nanf("");
-    if (threadIdx.x == 0 && a.entropy) a.entropy[row] = lost ? nan : some ? log_s - 2.0f * s.inv_t * (U / S) : 0.0f;
-    for (uint32_t g = 0; g < a.n_given; ++g) {
-        const int32_t c = a.given[row * a.n_given + g];
-        const float at = c >= 0 ? logit(x, allowed, (uint32_t)c, n) : kNone;
-        const bool there = at != kNone;
-        if (a.given_ranks) {
-            uint32_t in_front = 0;
-            if (there && !lost)
-                for (uint32_t d = threadIdx.x; d < n; d += 256) {
-                    const float v = logit(x, allowed, d, n);
-                    in_front += v > at || (v == at && d < (uint32_t)c);
+        if (a.given_ranks)
+            for (uint32_t g = 0; g < a.n_given; ++g) {
+                const float at = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, given_x), g));
+                const uint32_t c = (uint32_t)__builtin_amdgcn_readlane(given, g);
+                uint32_t count = 0;
+                if (c < base) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kPer; ++i) count += (uint32_t)__popcll(__ballot(v[i] > at));
+                } else if (c >= base + kChunk) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kPer; ++i) count += (uint32_t)__popcll(__ballot(v[i] >= at));
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < kPer; ++i)
+                        count += (uint32_t)__popcll(__ballot(v[i] > at || (v[i] == at && Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec < c)));
                 }
-            in_front = over_workgroup(in_front, (uint32_t*)fl, [](uint32_t p, uint32_t q) { return p + q; });
-            if (threadIdx.x == 0) a.given_ranks[row * a.n_given + g] = there && !lost ? (int32_t)in_front : -1;
-        }
-        if (threadIdx.x == 0 && a.given_logprobs) a.given_logprobs[row * a.n_given + g] = !there ? kNone : lost ? nan : log_prob(at, m, s.inv_t, log_s);
-    }
-    uint64_t below = ~0ull;
-    for (uint32_t k = 0; k < a.top; ++k) {
-        uint64_t best = 0;
-        if (some && !lost)
-            for (uint32_t c = threadIdx.x; c < n; c += 256) {
-                const uint64_t key = order_key(logit(x, allowed, c, n), c);
-                if (key < below && key > best) best = key;
+                if (lane == g) w.in_front += count;
             }
-        best = over_workgroup(best, kl, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-        below = best;
-        if (threadIdx.x == 0) {
-            const uint32_t c = 0xffffffffu - (uint32_t)best;
-            if (a.top_ids) a.top_ids[row * a.top + k] = best ? (int32_t)c : -1;
-            if (a.top_logprobs) a.top_logprobs[row * a.top + k] = best ? log_prob((float)x[c], m, s.inv_t, log_s) : lost ? nan : kNone;
+        if constexpr (TOP) {
+            list.equal = __builtin_nanf("");
+            if (__ballot(most > list.bar)) {
+                if (list.n == 0) {
+                    const float bar = bar_of(most, a.top);
+                    if (bar > kNone) list.equal = list.bar = bar;
+                }
+                uint32_t passing = 0;
+#pragma unroll
+                for (uint32_t i = 0; i < kPer; ++i) passing += (uint32_t)__popcll(__ballot(list.keeps(v[i])));
+                if (list.n + passing > kList - 4 && list.n > a.top) {
+                    list.cut(a.top, lane);
+                    list.equal = __builtin_nanf("");          // (all of it is in front of this chunk)
+                    passing = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < kPer; ++i) passing += (uint32_t)__popcll(__ballot(list.keeps(v[i])));
+                }
+                if (list.n + passing <= kList - 4) {
+#pragma unroll
+                    for (uint32_t i = 0; i < kPer; ++i)
+                        list.append(list.keeps(v[i]), order_key(v[i], Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
+                } else {
+#pragma nounroll
+                    for (uint32_t i = 0; i < kPer; ++i) {
+                        float one = v[0];
+#pragma unroll
+                        for (uint32_t j = 1; j < kPer; ++j) if (j == i) one = v[j];
+                        if (list.n > kListRoom) list.cut(a.top, lane);
+                        list.append(list.keeps(one), order_key(one, Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
+                    }
+                }
+            }
         }
     }
+    w.sums.over_wave(s.exp2_scale);
+    if constexpr (TOP) list.cut(a.top, lane);
+
+    if constexpr (WAVES > 1) {
+        __shared__ Sums wave_sums[WAVES];
+        __shared__ uint32_t wave_n[WAVES], wave_front[WAVES][MT_SCORE_MAX_GIVEN], last;
+        // the waves' shares to wave 0
+        const auto join_waves = [&]() {
+            if (lane == 0) { wave_sums[wave] = w.sums; wave_n[wave] = list.n; }
+            if (lane < MT_SCORE_MAX_GIVEN) wave_front[wave][lane] = w.in_front;
+            __syncthreads();
+            if (wave != 0) return;
+            for (uint32_t o = 1; o < WAVES; ++o) {
+                w.sums.join(wave_sums[o], s.exp2_scale);
+                if (lane < MT_SCORE_MAX_GIVEN) w.in_front += wave_front[o][lane];
+                if constexpr (TOP) { if (lane < wave_n[o]) list.at[list.n + lane] = lists[o][lane]; list.n += wave_n[o]; }
+            }
+            if constexpr (TOP) list.cut(a.top, lane);
+        };
+        join_waves();
+        if (s.parts > 1) {
+            // the last workgroup of a row to come here joins the parts of all of them
+            uint32_t* tickets = (uint32_t*)a.scratch;
+            Part* parts = (Part*)((uint8_t*)a.scratch + kSplitRows * 4) + (uint64_t)row * s.parts;
+            if (wave == 0) {
+                Part& p = parts[part];
+                if (lane == 0) { p.m = w.sums.m; p.s = w.sums.s; p.u = w.sums.u; }
+                if (lane < a.n_given) p.in_front[lane] = w.in_front;
+                if constexpr (TOP) if (lane < a.top) p.keys[lane] = lane < list.n ? list.at[lane] : 0;
+                __threadfence();
+                if (lane == 0) last = atomicAdd(&tickets[row], 1u) == s.parts - 1;
+            }
+            __syncthreads();
+            if (!last) return;
+            __threadfence();
+            if (threadIdx.x == 0) tickets[row] = 0;               // ready for the next call
+            // wave v takes parts v, v + 4, ..., a lane each; of their keys every lane takes some
+            w = Share{{kLowest, 0.0f, 0.0f}, 0};
+            const uint32_t mine = (s.parts - wave + WAVES - 1) / WAVES;
+            uint64_t keys[kPartKeys];
+            if constexpr (TOP) {
+#pragma unroll
+                for (uint32_t j = 0; j < kPartKeys; ++j) {
+                    const uint32_t i = 64 * j + lane;
+                    keys[j] = i < mine * a.top ? parts[wave + i / a.top * WAVES].keys[i % a.top] : 0;
+                }
+            }
+            const bool has = lane < mine;
+            const Part& p = parts[has ? wave + lane * WAVES : 0];
+            if (has) w.sums = Sums{p.m, p.s, p.u};
+            if (a.given_ranks)
+                for (uint32_t g = 0; g < a.n_given; ++g) {
+                    uint32_t count = has ? p.in_front[g] : 0;
+#pragma unroll
+                    for (int d = 1; d < 64; d *= 2) count += __shfl_xor(count, d);
+                    if (lane == g) w.in_front = count;
+                }
+            w.sums.over_wave(s.exp2_scale);
+            if constexpr (TOP) {
+                list.n = 0;
+                float most = kNone;
+#pragma unroll
+                for (uint32_t j = 0; j < kPartKeys; ++j) if (keys[j]) most = fmaxf(most, key_logit(keys[j]));
+                float bar = bar_of(most, a.top);
+#pragma unroll
+                for (uint32_t j = 0; j < kPartKeys; ++j) {
+                    if (list.n > kListRoom) { list.cut(a.top, lane); bar = list.bar; }
+                    list.append(keys[j] && key_logit(keys[j]) >= bar, keys[j]);
+                }
+            }
+            if constexpr (TOP) list.cut(a.top, lane);
+            __syncthreads();
+            join_waves();
+        }
+        if (wave != 0) return;
+    }
+
+    // (the largest logit's own term is 1: without a class the sum is 0, with a NaN or +infinity among them it is NaN)
+    const bool some = w.sums.s != 0.0f, lost = some && !(w.sums.s < __builtin_inff());
+    const float log_s = logf(w.sums.s), nan = __builtin_nanf("");
+    if (lane == 0 && a.entropy) a.entropy[row] = lost ? nan : some ? log_s - 2.0f * s.inv_t * (w.sums.u / w.sums.s) : 0.0f;
+    if (lane < a.n_given) {
+        const bool there = given_x != kNone;
+        const uint64_t to = (uint64_t)row * a.n_given + lane;
+        if (a.given_logprobs) a.given_logprobs[to] = !there ? kNone : lost ? nan : log_prob(given_x, w.sums.m, s.inv_t, log_s);
+        if (a.given_ranks) a.given_ranks[to] = there && !lost ? (int32_t)w.in_front : -1;
+    }
+    if constexpr (TOP) {
+        if (lane < a.top) {
+            const uint64_t key = lane < list.n && !lost ? list.at[lane] : 0;
+            const uint64_t to = (uint64_t)row * a.top + lane;
+            if (a.top_ids) a.top_ids[to] = key ? key_class(key) : -1;
+            if (a.top_logprobs) a.top_logprobs[to] = key ? log_prob(key_logit(key), w.sums.m, s.inv_t, log_s) : lost ? nan : kNone;
+        }
+    }
+}
+
+template <typename T, bool TOP, bool MASK>
+hipError_t go(const ScoreArgs& s, hipStream_t st)
+{
+    if (s.parts == 1 && s.a.classes <= 2 * kChunk)
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(256), 0, st, s);
+    else
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves>), dim3(s.a.rows, s.parts), dim3(256), 0, st, s);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t choose(const ScoreArgs& s, hipStream_t st)
+{
+    const bool top = s.a.top_ids || s.a.top_logprobs, mask = s.a.allowed != nullptr;
+    if (top) return mask ? go<T, true, true>(s, st) : go<T, true, false>(s, st);
+    return mask ? go<T, false, true>(s, st) : go<T, false, false>(s, st);
 }
 
 }  // namespace
 
-void score_split(uint32_t, uint32_t classes, uint32_t* parts, uint32_t* part_len) { *parts = 1; *part_len = classes; }
-uint64_t score_scratch_bytes(uint32_t, uint32_t, uint32_t, uint32_t) { return 0; }
+// A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.
+void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len)
+{
+    *parts = 1; *part_len = classes;
+    if (rows == 0 || rows > kSplitRows / 2) return;
+    const uint32_t span = kChunk * kWaves, want = std::min(kMaxParts, kSplitRows / rows);
+    const uint32_t spans = (classes + span - 1) / span;
+    if (spans < 2 || want < 2) return;
+    *part_len = (spans + want - 1) / want * span;
+    *parts = (uint32_t)(((uint64_t)classes + *part_len - 1) / *part_len);
+}
+
+uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t, uint32_t)
+{
+    uint32_t parts, part_len;
+    score_split(rows, classes, &parts, &part_len);
+    return parts > 1 ? kSplitRows * (4 + sizeof(Part)) : 0;      // rows x parts is never more than that
+}
 
 hipError_t launch_score(const ScoreArgs& a, hipStream_t s)
 {
-    if (a.a.dtype == MT_BF16) hipLaunchKernelGGL((score_kernel<__bf16>), dim3(a.a.rows), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((score_kernel<float>), dim3(a.a.rows), dim3(256), 0, s, a);
-    return hipGetLastError();
+    return a.a.dtype == MT_BF16 ? choose<__bf16>(a, s) : choose<float>(a, s);
 }
 
 }  // namespace mt
