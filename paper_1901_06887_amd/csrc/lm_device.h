@@ -58,12 +58,29 @@ template <typename T> __device__ __forceinline__ void store_some(T* p, uint32_t 
     for (uint32_t i = 0; i < 8; ++i) if (i < n) p[i] = (T)v[i];
 }
 
-// Sum over the wave, in every lane.
-__device__ __forceinline__ float wave_sum(float v)
+// Over the wave, in every lane, by data-parallel-primitive moves (no LDS traffic): shifts by 1, 2, 4, 8 inside rows of 16 lanes, lane 15
+// of a row to the next, lane 31 to the upper half; the last lane has it all.
+template <typename F> __device__ __forceinline__ uint32_t wave_fold(uint32_t v, F f)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    return v;
+#define MT_FOLD(ctrl, rows) v = f(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false))
+    MT_FOLD(0x111, 0xf); MT_FOLD(0x112, 0xf); MT_FOLD(0x114, 0xf); MT_FOLD(0x118, 0xf); MT_FOLD(0x142, 0xa); MT_FOLD(0x143, 0xc);
+#undef MT_FOLD
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+// (lanes without a source get 0, which adds nothing)
+__device__ __forceinline__ float wave_total(float v)
+{
+    return __builtin_bit_cast(float, wave_fold(__builtin_bit_cast(uint32_t, v), [](uint32_t a, uint32_t b) {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, a) + __builtin_bit_cast(float, b)); }));
+}
+__device__ __forceinline__ uint32_t wave_total(uint32_t v) { return wave_fold(v, [](uint32_t a, uint32_t b) { return a + b; }); }
+// The largest; NaN only if all are.  (As integers in the order of the values, above 0.)
+__device__ __forceinline__ float wave_max(float v)
+{
+    uint32_t b = __builtin_bit_cast(uint32_t, v);
+    b = v == v ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0;
+    b = wave_fold(b, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+    return b == 0 ? __builtin_nanf("") : __builtin_bit_cast(float, b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 
 }  // namespace mt

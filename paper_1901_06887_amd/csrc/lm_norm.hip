@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(THREADS == 64 ? 256 : THREADS) norm_kernel(mt_
 #pragma unroll
             for (uint32_t i = 0; i < kRun; ++i) squares = fmaf(h[j][i], h[j][i], squares);
     }
-    squares = wave_sum(squares);
+    squares = wave_total(squares);
     if constexpr (THREADS > 64) {
         __shared__ float part[THREADS / 64];
         if ((t & 63) == 0) part[t >> 6] = squares;

@@ -22,12 +22,16 @@ constexpr uint32_t kSplitRows = 1024;             // most rows whose classes wor
 constexpr uint32_t kMaxParts = 64;                // most workgroups that share one
 constexpr uint32_t kPartKeys = kMaxParts / kWaves * MT_SCORE_MAX_TOP / 64;      // keys of a lane where parts are joined
 
-// What a workgroup hands over of its share of a row.
+// What a workgroup hands over of its share of a row, to another one on any XCD: every word is stored through to memory and loaded from there
+// (agent scope), and the ticket is drawn when the stores have arrived.  Fences of the whole L2 in their place took 4 us more.
 struct Part {
-    float m, s, u; uint32_t pad;
+    float m, s, u, pad;
     uint32_t in_front[MT_SCORE_MAX_GIVEN];
     uint64_t keys[MT_SCORE_MAX_TOP];
 };
+
+template <typename V> __device__ __forceinline__ void hand_over(V* p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V> __device__ __forceinline__ V take_over(const V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // A class's logit, -infinity where it is not allowed.
 template <typename T>
@@ -75,8 +79,8 @@ struct Sums {
     }
     __device__ __forceinline__ void over_wave(float scale)
     {
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) join(Sums{__shfl_xor(m, d), __shfl_xor(s, d), __shfl_xor(u, d)}, scale);
+        rebase(wave_max(m), scale);
+        s = wave_total(s); u = wave_total(u);
     }
 };
 
@@ -87,9 +91,19 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_wave_barrier();
 }
 
+// Entries among the kStep at `at` that are in front of `key`.
+constexpr uint32_t kStep = 8;
+__device__ __forceinline__ uint32_t in_front_of(uint64_t key, const uint64_t* at)
+{
+    uint32_t n = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kStep; ++k) n += at[k] > key;
+    return n;
+}
+
 // Entries of a wave's list, and the bar: a class is kept if its logit is above `bar`, or equal to `equal` (NaN: to nothing).
 struct List {
-    uint64_t* at;         // LDS, kList entries
+    uint64_t* at;         // LDS, kList entries and kStep more
     uint32_t n;
     float bar, equal;
     __device__ __forceinline__ bool keeps(float x) const { return x > bar || x == equal; }
@@ -97,28 +111,22 @@ struct List {
     // The best `top` of the entries, in order; raises the bar to the last of them.
     __device__ __forceinline__ void cut(uint32_t top, uint32_t lane)
     {
-        if (lane < 4) at[n + lane] = 0;           // (the loop below takes four at a time; the list has room for them)
+        if (lane < kStep) at[n + lane] = 0;
         wave_sync();
         uint64_t own[kList / 64];
-        uint32_t before[kList / 64];
+        uint32_t before[kList / 64] = {};
 #pragma unroll
-        for (uint32_t j = 0; j < kList / 64; ++j) { own[j] = 64 * j + lane < n ? at[64 * j + lane] : 0; before[j] = own[j] ? 0 : kList; }
+        for (uint32_t j = 0; j < kList / 64; ++j) own[j] = 64 * j + lane < n ? at[64 * j + lane] : 0;
         if (n <= 64) {
-            for (uint32_t i = 0; i < n; i += 4)
-#pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) before[0] += at[i + k] > own[0];
+            for (uint32_t i = 0; i < n; i += kStep) before[0] += in_front_of(own[0], at + i);
         } else {
-            for (uint32_t i = 0; i < n; i += 4)
+            for (uint32_t i = 0; i < n; i += kStep)
 #pragma unroll
-                for (uint32_t k = 0; k < 4; ++k) {
-                    const uint64_t e = at[i + k];
-#pragma unroll
-                    for (uint32_t j = 0; j < kList / 64; ++j) before[j] += e > own[j];
-                }
+                for (uint32_t j = 0; j < kList / 64; ++j) before[j] += in_front_of(own[j], at + i);
         }
         wave_sync();
 #pragma unroll
-        for (uint32_t j = 0; j < kList / 64; ++j) if (before[j] < top) at[before[j]] = own[j];
+        for (uint32_t j = 0; j < kList / 64; ++j) if (own[j] && before[j] < top) at[before[j]] = own[j];
         wave_sync();
         if (n >= top) {
             n = top;
@@ -133,17 +141,17 @@ struct List {
         n += (uint32_t)__popcll(lanes);
     }
 };
-constexpr uint32_t kListRoom = kList - 64 - 4;    // entries after which every lane can still append one
+constexpr uint32_t kListRoom = kList - 64;    // entries after which every lane can still append one
 
 // The top-th largest of the lanes' values, rounded down a little; -infinity if there are not so many.
 __device__ __forceinline__ float bar_of(float v, uint32_t top)
 {
-    // by bits from the highest, over values ordered as integers; 20 of them decide
+    // by bits from the highest, over values ordered as integers; 16 of them decide
     uint32_t b = __builtin_bit_cast(uint32_t, v);
     b = v == kNone ? 0 : b & 0x80000000u ? ~b : b | 0x80000000u;
     uint32_t found = 0;
 #pragma unroll
-    for (int bit = 31; bit >= 12; --bit) {
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t probe = found | 1u << bit;
         if ((uint32_t)__popcll(__ballot(b >= probe)) >= top) found = probe;
     }
@@ -232,7 +240,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t row = WAVES == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
     if (row >= a.rows) return;                    // (whole waves, and none where a barrier follows)
-    __shared__ __attribute__((aligned(16))) uint64_t lists[TOP ? kWaves : 1][TOP ? kList : 1];
+    __shared__ __attribute__((aligned(16))) uint64_t lists[TOP ? kWaves : 1][TOP ? kList + kStep : 1];
     const T* x = (const T*)a.logits + row * a.row_stride;
     const uint32_t* allowed = MASK ? a.allowed + row * a.allowed_stride : nullptr;
     const uint32_t part = WAVES == 1 ? 0 : blockIdx.y;
@@ -293,14 +301,14 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
                 uint32_t passing = 0;
 #pragma unroll
                 for (uint32_t i = 0; i < kPer; ++i) passing += (uint32_t)__popcll(__ballot(list.keeps(v[i])));
-                if (list.n + passing > kList - 4 && list.n > a.top) {
+                if (list.n + passing > kList && list.n > a.top) {
                     list.cut(a.top, lane);
                     list.equal = __builtin_nanf("");          // (all of it is in front of this chunk)
                     passing = 0;
 #pragma unroll
                     for (uint32_t i = 0; i < kPer; ++i) passing += (uint32_t)__popcll(__ballot(list.keeps(v[i])));
                 }
-                if (list.n + passing <= kList - 4) {
+                if (list.n + passing <= kList) {
 #pragma unroll
                     for (uint32_t i = 0; i < kPer; ++i)
                         list.append(list.keeps(v[i]), order_key(v[i], Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
@@ -323,18 +331,34 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     if constexpr (WAVES > 1) {
         __shared__ Sums wave_sums[WAVES];
         __shared__ uint32_t wave_n[WAVES], wave_front[WAVES][MT_SCORE_MAX_GIVEN], last;
-        // the waves' shares to wave 0
+        __shared__ __attribute__((aligned(16))) uint64_t joined[TOP ? MT_SCORE_MAX_TOP : 1];
+        // the waves' shares to wave 0; of the lists, each in order, every entry finds its place by those in front of it in the others
         const auto join_waves = [&]() {
             if (lane == 0) { wave_sums[wave] = w.sums; wave_n[wave] = list.n; }
             if (lane < MT_SCORE_MAX_GIVEN) wave_front[wave][lane] = w.in_front;
+            if constexpr (TOP) if (lane >= list.n && lane < MT_SCORE_MAX_TOP) list.at[lane] = 0;
             __syncthreads();
+            uint32_t n = 0;
+            if constexpr (TOP) {
+                const uint64_t own = lane < list.n ? list.at[lane] : 0;
+                uint32_t before = lane;
+#pragma unroll
+                for (uint32_t o = 0; o < WAVES; ++o) {
+                    n += wave_n[o];
+                    if (o != wave)
+                        for (uint32_t i = 0; i < wave_n[o]; i += kStep) before += in_front_of(own, lists[o] + i);
+                }
+                if (own && before < a.top) joined[before] = own;
+                n = min(n, a.top);
+                __syncthreads();
+            }
             if (wave != 0) return;
+#pragma unroll
             for (uint32_t o = 1; o < WAVES; ++o) {
                 w.sums.join(wave_sums[o], s.exp2_scale);
                 if (lane < MT_SCORE_MAX_GIVEN) w.in_front += wave_front[o][lane];
-                if constexpr (TOP) { if (lane < wave_n[o]) list.at[list.n + lane] = lists[o][lane]; list.n += wave_n[o]; }
             }
-            if constexpr (TOP) list.cut(a.top, lane);
+            if constexpr (TOP) { list.at = joined; list.n = n; }
         };
         join_waves();
         if (s.parts > 1) {
@@ -343,16 +367,15 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
             Part* parts = (Part*)((uint8_t*)a.scratch + kSplitRows * 4) + (uint64_t)row * s.parts;
             if (wave == 0) {
                 Part& p = parts[part];
-                if (lane == 0) { p.m = w.sums.m; p.s = w.sums.s; p.u = w.sums.u; }
-                if (lane < a.n_given) p.in_front[lane] = w.in_front;
-                if constexpr (TOP) if (lane < a.top) p.keys[lane] = lane < list.n ? list.at[lane] : 0;
-                __threadfence();
-                if (lane == 0) last = atomicAdd(&tickets[row], 1u) == s.parts - 1;
+                if (lane == 0) { hand_over(&p.m, w.sums.m); hand_over(&p.s, w.sums.s); hand_over(&p.u, w.sums.u); }
+                if (lane < a.n_given) hand_over(&p.in_front[lane], w.in_front);
+                if constexpr (TOP) if (lane < a.top) hand_over(&p.keys[lane], lane < list.n ? list.at[lane] : 0);
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                if (lane == 0) last = __hip_atomic_fetch_add(&tickets[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == s.parts - 1;
             }
             __syncthreads();
             if (!last) return;
-            __threadfence();
-            if (threadIdx.x == 0) tickets[row] = 0;               // ready for the next call
+            if (threadIdx.x == 0) hand_over(&tickets[row], 0u);   // ready for the next call
             // wave v takes parts v, v + 4, ..., a lane each; of their keys every lane takes some
             w = Share{{kLowest, 0.0f, 0.0f}, 0};
             const uint32_t mine = (s.parts - wave + WAVES - 1) / WAVES;
@@ -361,22 +384,20 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
 #pragma unroll
                 for (uint32_t j = 0; j < kPartKeys; ++j) {
                     const uint32_t i = 64 * j + lane;
-                    keys[j] = i < mine * a.top ? parts[wave + i / a.top * WAVES].keys[i % a.top] : 0;
+                    keys[j] = i < mine * a.top ? take_over(&parts[wave + i / a.top * WAVES].keys[i % a.top]) : 0;
                 }
             }
             const bool has = lane < mine;
             const Part& p = parts[has ? wave + lane * WAVES : 0];
-            if (has) w.sums = Sums{p.m, p.s, p.u};
+            if (has) w.sums = Sums{take_over(&p.m), take_over(&p.s), take_over(&p.u)};
             if (a.given_ranks)
                 for (uint32_t g = 0; g < a.n_given; ++g) {
-                    uint32_t count = has ? p.in_front[g] : 0;
-#pragma unroll
-                    for (int d = 1; d < 64; d *= 2) count += __shfl_xor(count, d);
+                    const uint32_t count = wave_total(has ? take_over(&p.in_front[g]) : 0u);
                     if (lane == g) w.in_front = count;
                 }
             w.sums.over_wave(s.exp2_scale);
             if constexpr (TOP) {
-                list.n = 0;
+                list = List{lists[wave], 0, kNone, __builtin_nanf("")};
                 float most = kNone;
 #pragma unroll
                 for (uint32_t j = 0; j < kPartKeys; ++j) if (keys[j]) most = fmaxf(most, key_logit(keys[j]));
