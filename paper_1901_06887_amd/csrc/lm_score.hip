@@ -101,37 +101,33 @@ __device__ __forceinline__ uint32_t in_front_of(uint64_t key, const uint64_t* at
     return n;
 }
 
-// Entries of a wave's list, and the bar: a class is kept if its logit is above `bar`, or equal to `equal` (NaN: to nothing).
+// Entries of a wave's list in no order, and the bar: a class is kept if its logit is above `bar`, or equal to `equal` (NaN: to nothing).
+// (The code is kept short, in loops: a call runs it once, so much of its time is the fetch of the code.)
 struct List {
     uint64_t* at;         // LDS, kList entries and kStep more
+    uint64_t* best;       // LDS, MT_SCORE_MAX_TOP entries
     uint32_t n;
     float bar, equal;
     __device__ __forceinline__ bool keeps(float x) const { return x > bar || x == equal; }
 
-    // The best `top` of the entries, in order; raises the bar to the last of them.
+    // Leaves the best `top` of the entries, in order, and raises the bar to the last of them.
     __device__ __forceinline__ void cut(uint32_t top, uint32_t lane)
     {
         if (lane < kStep) at[n + lane] = 0;
         wave_sync();
-        uint64_t own[kList / 64];
-        uint32_t before[kList / 64] = {};
-#pragma unroll
-        for (uint32_t j = 0; j < kList / 64; ++j) own[j] = 64 * j + lane < n ? at[64 * j + lane] : 0;
-        if (n <= 64) {
-            for (uint32_t i = 0; i < n; i += kStep) before[0] += in_front_of(own[0], at + i);
-        } else {
-            for (uint32_t i = 0; i < n; i += kStep)
-#pragma unroll
-                for (uint32_t j = 0; j < kList / 64; ++j) before[j] += in_front_of(own[j], at + i);
+#pragma nounroll
+        for (uint32_t j = 0; j < n; j += 64) {
+            const uint64_t own = j + lane < n ? at[j + lane] : 0;
+            uint32_t before = 0;
+#pragma nounroll
+            for (uint32_t i = 0; i < n; i += kStep) before += in_front_of(own, at + i);
+            if (own && before < top) best[before] = own;
         }
         wave_sync();
-#pragma unroll
-        for (uint32_t j = 0; j < kList / 64; ++j) if (own[j] && before[j] < top) at[before[j]] = own[j];
+        if (n > top) n = top;
+        if (lane < n) at[lane] = best[lane];
         wave_sync();
-        if (n >= top) {
-            n = top;
-            equal = bar = key_logit(at[top - 1]);
-        }
+        if (n == top) equal = bar = key_logit(at[top - 1]);
     }
 
     __device__ __forceinline__ void append(bool keep, uint64_t key)
@@ -141,7 +137,7 @@ struct List {
         n += (uint32_t)__popcll(lanes);
     }
 };
-constexpr uint32_t kListRoom = kList - 64;    // entries after which every lane can still append one
+constexpr uint32_t kListRoom = kList - 64;        // entries up to which every lane can still append one
 
 // The top-th largest of the lanes' values, rounded down a little; -infinity if there are not so many.
 __device__ __forceinline__ float bar_of(float v, uint32_t top)
@@ -150,7 +146,7 @@ __device__ __forceinline__ float bar_of(float v, uint32_t top)
     uint32_t b = __builtin_bit_cast(uint32_t, v);
     b = v == kNone ? 0 : b & 0x80000000u ? ~b : b | 0x80000000u;
     uint32_t found = 0;
-#pragma unroll
+#pragma nounroll
     for (int bit = 31; bit >= 16; --bit) {
         const uint32_t probe = found | 1u << bit;
         if ((uint32_t)__popcll(__ballot(b >= probe)) >= top) found = probe;
@@ -241,6 +237,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     const uint32_t row = WAVES == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
     if (row >= a.rows) return;                    // (whole waves, and none where a barrier follows)
     __shared__ __attribute__((aligned(16))) uint64_t lists[TOP ? kWaves : 1][TOP ? kList + kStep : 1];
+    __shared__ __attribute__((aligned(16))) uint64_t best[TOP ? kWaves : 1][TOP ? MT_SCORE_MAX_TOP : 1];
     const T* x = (const T*)a.logits + row * a.row_stride;
     const uint32_t* allowed = MASK ? a.allowed + row * a.allowed_stride : nullptr;
     const uint32_t part = WAVES == 1 ? 0 : blockIdx.y;
@@ -257,7 +254,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     const float given_x = given >= 0 ? logit(x, allowed, (uint32_t)given, n) : kNone;
 
     Share w{{kLowest, 0.0f, 0.0f}, 0};
-    List list{TOP ? lists[wave] : nullptr, 0, kNone, __builtin_nanf("")};
+    List list{TOP ? lists[wave] : nullptr, TOP ? best[wave] : nullptr, 0, kNone, __builtin_nanf("")};
     for (; base < end; base += kChunk) {
         float v[kPer];
         raw.template logits<MASK>(v, base, lane, end);
@@ -292,76 +289,70 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
                 if (lane == g) w.in_front += count;
             }
         if constexpr (TOP) {
-            list.equal = __builtin_nanf("");
-            if (__ballot(most > list.bar)) {
-                if (list.n == 0) {
+            list.equal = __builtin_nanf("");      // what is in the list is in front of an equal class of this chunk
+            const uint64_t lanes = __ballot(most > list.bar);
+            if (lanes) {
+                if ((uint32_t)__popcll(lanes) >= a.top) {
                     const float bar = bar_of(most, a.top);
-                    if (bar > kNone) list.equal = list.bar = bar;
+                    if (bar > list.bar) list.equal = list.bar = bar;
                 }
-                uint32_t passing = 0;
+                uint32_t mine = 0;
 #pragma unroll
-                for (uint32_t i = 0; i < kPer; ++i) passing += (uint32_t)__popcll(__ballot(list.keeps(v[i])));
-                if (list.n + passing > kList && list.n > a.top) {
-                    list.cut(a.top, lane);
-                    list.equal = __builtin_nanf("");          // (all of it is in front of this chunk)
-                    passing = 0;
-#pragma unroll
-                    for (uint32_t i = 0; i < kPer; ++i) passing += (uint32_t)__popcll(__ballot(list.keeps(v[i])));
-                }
-                if (list.n + passing <= kList) {
-#pragma unroll
-                    for (uint32_t i = 0; i < kPer; ++i)
-                        list.append(list.keeps(v[i]), order_key(v[i], Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
-                } else {
+                for (uint32_t i = 0; i < kPer; ++i) mine |= list.keeps(v[i]) ? 1u << i : 0;
 #pragma nounroll
-                    for (uint32_t i = 0; i < kPer; ++i) {
-                        float one = v[0];
+                while (__ballot(mine != 0)) {
+                    const uint32_t i = mine ? __builtin_ctz(mine) : 0;
+                    float one = v[0];
 #pragma unroll
-                        for (uint32_t j = 1; j < kPer; ++j) if (j == i) one = v[j];
-                        if (list.n > kListRoom) list.cut(a.top, lane);
-                        list.append(list.keeps(one), order_key(one, Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
-                    }
+                    for (uint32_t j = 1; j < kPer; ++j) one = i == j ? v[j] : one;
+                    if (list.n > kListRoom) list.cut(a.top, lane);
+                    list.append(mine != 0 && list.keeps(one), order_key(one, Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
+                    mine &= mine - 1;
                 }
             }
         }
     }
     w.sums.over_wave(s.exp2_scale);
-    if constexpr (TOP) list.cut(a.top, lane);
-
-    if constexpr (WAVES > 1) {
-        __shared__ Sums wave_sums[WAVES];
-        __shared__ uint32_t wave_n[WAVES], wave_front[WAVES][MT_SCORE_MAX_GIVEN], last;
-        __shared__ __attribute__((aligned(16))) uint64_t joined[TOP ? MT_SCORE_MAX_TOP : 1];
-        // the waves' shares to wave 0; of the lists, each in order, every entry finds its place by those in front of it in the others
-        const auto join_waves = [&]() {
+    // The waves' shares to wave 0, the entries of all lists to their places; then, in a row of several parts, the same with what they handed over.
+    __shared__ Sums wave_sums[WAVES];
+    __shared__ uint32_t wave_n[WAVES], wave_front[WAVES][MT_SCORE_MAX_GIVEN], last;
+    for (bool parts_joined = s.parts == 1;; parts_joined = true) {
+        if constexpr (TOP) if (lane < kStep) list.at[list.n + lane] = 0;
+        if constexpr (WAVES > 1) {
             if (lane == 0) { wave_sums[wave] = w.sums; wave_n[wave] = list.n; }
             if (lane < MT_SCORE_MAX_GIVEN) wave_front[wave][lane] = w.in_front;
-            if constexpr (TOP) if (lane >= list.n && lane < MT_SCORE_MAX_TOP) list.at[lane] = 0;
             __syncthreads();
-            uint32_t n = 0;
-            if constexpr (TOP) {
-                const uint64_t own = lane < list.n ? list.at[lane] : 0;
-                uint32_t before = lane;
-#pragma unroll
+        } else wave_sync();
+        uint32_t n = list.n;
+        if constexpr (TOP) {
+            if constexpr (WAVES > 1) n = wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+            n = min(n, a.top);
+#pragma nounroll
+            for (uint32_t j = 0; j < list.n; j += 64) {
+                const uint64_t own = j + lane < list.n ? list.at[j + lane] : 0;
+                uint32_t before = 0;
+#pragma nounroll
                 for (uint32_t o = 0; o < WAVES; ++o) {
-                    n += wave_n[o];
-                    if (o != wave)
-                        for (uint32_t i = 0; i < wave_n[o]; i += kStep) before += in_front_of(own, lists[o] + i);
+                    const uint32_t others = WAVES > 1 ? wave_n[o] : list.n;
+#pragma nounroll
+                    for (uint32_t i = 0; i < others; i += kStep) before += in_front_of(own, lists[WAVES > 1 ? o : wave] + i);
                 }
-                if (own && before < a.top) joined[before] = own;
-                n = min(n, a.top);
-                __syncthreads();
+                if (own && before < a.top) best[WAVES > 1 ? 0 : wave][before] = own;
             }
-            if (wave != 0) return;
+            if constexpr (WAVES > 1) __syncthreads(); else wave_sync();
+        }
+        if constexpr (WAVES > 1) {
+            if (wave == 0) {
 #pragma unroll
-            for (uint32_t o = 1; o < WAVES; ++o) {
-                w.sums.join(wave_sums[o], s.exp2_scale);
-                if (lane < MT_SCORE_MAX_GIVEN) w.in_front += wave_front[o][lane];
+                for (uint32_t o = 1; o < WAVES; ++o) {
+                    w.sums.join(wave_sums[o], s.exp2_scale);
+                    if (lane < MT_SCORE_MAX_GIVEN) w.in_front += wave_front[o][lane];
+                }
             }
-            if constexpr (TOP) { list.at = joined; list.n = n; }
-        };
-        join_waves();
-        if (s.parts > 1) {
+        }
+        list.n = n;
+        if (parts_joined) break;
+        if constexpr (WAVES > 1) {
             // the last workgroup of a row to come here joins the parts of all of them
             uint32_t* tickets = (uint32_t*)a.scratch;
             Part* parts = (Part*)((uint8_t*)a.scratch + kSplitRows * 4) + (uint64_t)row * s.parts;
@@ -369,7 +360,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
                 Part& p = parts[part];
                 if (lane == 0) { hand_over(&p.m, w.sums.m); hand_over(&p.s, w.sums.s); hand_over(&p.u, w.sums.u); }
                 if (lane < a.n_given) hand_over(&p.in_front[lane], w.in_front);
-                if constexpr (TOP) if (lane < a.top) hand_over(&p.keys[lane], lane < list.n ? list.at[lane] : 0);
+                if constexpr (TOP) if (lane < a.top) hand_over(&p.keys[lane], lane < list.n ? best[0][lane] : 0);
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 if (lane == 0) last = __hip_atomic_fetch_add(&tickets[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == s.parts - 1;
             }
@@ -397,23 +388,24 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
                 }
             w.sums.over_wave(s.exp2_scale);
             if constexpr (TOP) {
-                list = List{lists[wave], 0, kNone, __builtin_nanf("")};
+                list.n = 0; list.bar = kNone;
                 float most = kNone;
 #pragma unroll
                 for (uint32_t j = 0; j < kPartKeys; ++j) if (keys[j]) most = fmaxf(most, key_logit(keys[j]));
-                float bar = bar_of(most, a.top);
+                list.equal = list.bar = bar_of(most, a.top);
+#pragma nounroll
+                for (uint32_t j = 0; j * 64 < mine * a.top; ++j) {
+                    uint64_t one = keys[0];
 #pragma unroll
-                for (uint32_t j = 0; j < kPartKeys; ++j) {
-                    if (list.n > kListRoom) { list.cut(a.top, lane); bar = list.bar; }
-                    list.append(keys[j] && key_logit(keys[j]) >= bar, keys[j]);
+                    for (uint32_t k = 1; k < kPartKeys; ++k) one = j == k ? keys[k] : one;
+                    if (list.n > kListRoom) list.cut(a.top, lane);
+                    list.append(one && list.keeps(key_logit(one)), one);
                 }
+                __syncthreads();                  // (the lists and `best` are read no more)
             }
-            if constexpr (TOP) list.cut(a.top, lane);
-            __syncthreads();
-            join_waves();
         }
-        if (wave != 0) return;
     }
+    if (WAVES > 1 && wave != 0) return;
 
     // (the largest logit's own term is 1: without a class the sum is 0, with a NaN or +infinity among them it is NaN)
     const bool some = w.sums.s != 0.0f, lost = some && !(w.sums.s < __builtin_inff());
@@ -427,7 +419,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     }
     if constexpr (TOP) {
         if (lane < a.top) {
-            const uint64_t key = lane < list.n && !lost ? list.at[lane] : 0;
+            const uint64_t key = lane < list.n && !lost ? best[WAVES > 1 ? 0 : wave][lane] : 0;
             const uint64_t to = (uint64_t)row * a.top + lane;
             if (a.top_ids) a.top_ids[to] = key ? key_class(key) : -1;
             if (a.top_logprobs) a.top_logprobs[to] = key ? log_prob(key_logit(key), w.sums.m, s.inv_t, log_s) : lost ? nan : kNone;
