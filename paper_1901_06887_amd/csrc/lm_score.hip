@@ -447,16 +447,19 @@ hipError_t choose(const ScoreArgs& s, hipStream_t st)
 
 }  // namespace
 
-// A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.
+// A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.  Handing over costs
+// some 4 us, a chunk more for every wave 1.7: two parts do not pay (64 rows of 8192 classes, 5 alternatives: 9.9 us whole, 11.2 in two parts; one row of
+// 10000 10.7 whole, 12.3 in two, 10.2 in three; 16 rows of 65001 60.6 whole, 34.9 in four, 17.4 in 16; 256 rows of 32768 23.9 whole, 20.9 in four).
 void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len)
 {
     *parts = 1; *part_len = classes;
     if (rows == 0 || rows > kSplitRows / 2) return;
     const uint32_t span = kChunk * kWaves, want = std::min(kMaxParts, kSplitRows / rows);
     const uint32_t spans = (classes + span - 1) / span;
-    if (spans < 2 || want < 2) return;
+    if (spans < 3 || want < 3) return;
     *part_len = (spans + want - 1) / want * span;
     *parts = (uint32_t)(((uint64_t)classes + *part_len - 1) / *part_len);
+    if (*parts < 3) *parts = 1, *part_len = classes;
 }
 
 uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t, uint32_t)
