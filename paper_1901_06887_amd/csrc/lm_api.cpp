@@ -164,11 +164,11 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
     if (most_rows == 0) return MT_OK;
     LM_TRY(c, hipSetDevice(v.device));
 
-    const Linear4Shape shape = linear4_shape(tiles, least_kt, most_rows, v.n_cus);
+    const Linear4Shape shape = linear4_shape(tiles, least_kt, most_rows, v.n_cus, a->x_dtype);
     Linear4Args k;
     k.arena = v.arena; k.x = a->x; k.x_scales = a->x_scales; k.y = a->y;
     k.x_stride = a->x_stride; k.x_scales_stride = a->x_scales_stride; k.y_stride = a->y_stride;
-    k.act = a->act; k.n_groups = 0;
+    k.act = a->act; k.n_groups = 0; k.y_bf16 = a->y_dtype == MT_BF16;
     uint64_t grid = 0;
     for (uint32_t g = 0; g < n_groups; ++g) {
         const mt_row_group& r = groups[g];
@@ -177,13 +177,13 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
         const uint64_t wgs = (uint64_t)div_up(m.N, kTile4Rows * shape.nt) * div_up(r.n_rows, kTile4Rows * shape.rt);
         if (wgs > kMaxGrid) return ctx_fail(c, MT_EUNSUPPORTED, "group %u takes %llu workgroups", g, (unsigned long long)wgs);
         if (k.n_groups == kGroups4 || grid + wgs > kMaxGrid) {
-            LM_TRY(c, launch_linear4(k, shape, a->x_dtype, a->y_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
+            LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
             k.n_groups = 0; grid = 0;
         }
         k.groups[k.n_groups++] = Group4{m.off, m.N, m.K, r.first_row, r.n_rows, (uint32_t)grid, m.has_bias ? 1u : 0u};
         grid += wgs;
     }
-    LM_TRY(c, launch_linear4(k, shape, a->x_dtype, a->y_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
+    LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
     return MT_OK;
 }
 

@@ -2,22 +2,19 @@
 //
 // y[i][n] = act(b[n] + sum_k W[n][k] x[i][k]).  The weights are the row operand of the 16x16x32 bf16 matrix instruction, 16 rows of x the
 // column operand: every e2m1 value times its scale is a bf16 value, every bf16 row value is itself one, an 8-bit one with its scale too, and an fp32
-// one is the sum of three; so the products are exact and the sums fp32.  Lane l of an operand holds output (or row) l % 16 and the 32 values of k
-// block l / 16, which is how the weights lie in memory: one 16-byte load a lane is an operand, with one scale, converted in place.
+// one is the sum of three; so the products are exact and the sums fp32.  (The instruction that multiplies 4-bit and 8-bit values with their scales itself
+// needs no conversions, but it keeps some 13 to 15 bits below the largest of the 128 products that it adds: blocks of small values vanish beside one of large ones.)
+//
+// Lane l of an operand holds output (or row) l % 16 and the 32 values of k block l / 16, which is how the weights lie in memory: one 16-byte load a lane
+// is an operand, with one scale.  Rows are read in place, in the same order; those that do not exist are taken from the last one that does, and their
+// columns of the product are never stored.
 #include "lm_device.h"
 
 namespace mt {
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-struct RowsF32 { };
-struct RowsBf16 { };
-struct RowsMx8 { };
-
-// 32 values of k of a row (a lane's share of a k tile) as matrix operands.
-template <typename X> struct Operand { static constexpr int kParts = 1; u32x4 v[1][4]; };
-template <> struct Operand<RowsF32> { static constexpr int kParts = 3; u32x4 v[3][4]; };
+enum Kind { kRowsF32, kRowsBf16, kRowsMx8 };
+constexpr uint32_t row_size(Kind k) { return k == kRowsF32 ? 4 : k == kRowsBf16 ? 2 : 1; }
 
 // fp32 as three bf16 values whose sum it is: the upper halves of what is left.  An infinity or NaN is the first alone.
 __device__ __forceinline__ void split3(float x, uint32_t (&part)[3])
@@ -32,81 +29,129 @@ __device__ __forceinline__ void split3(float x, uint32_t (&part)[3])
     if (special) { part[0] |= (b & 0xffffu) ? 0x400000u : 0u; part[1] = part[2] = 0; }
 }
 
-// A lane's 32 values from column `at` of a row of `width`; zeros past its end, and where the row does not exist.
-__device__ __forceinline__ void load_operand(Operand<RowsBf16>& o, const Linear4Args& a, uint64_t row, uint32_t at, uint32_t width, bool there)
-{
-    const __bf16* p = (const __bf16*)a.x + row * a.x_stride + at;
-    if (there && at + 32 <= width) {
+// A lane's 32 values of a row as they come from memory.
+template <Kind KIND> struct RawRow {
+    static constexpr uint32_t kVecs = row_size(KIND) * 2;      // of 16 bytes
+    u32x4 v[kVecs];
+    uint32_t scale;
+
+    // p: the lane's k block
+    __device__ __forceinline__ void load(const uint8_t* p, const uint8_t* scale_at)
+    {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o.v[0][j] = *(const Any<__bf16>::vec16*)(p + 8 * j);
-        return;
-    }
-    const uint32_t n = there && at < width ? width - at : 0;
-#pragma unroll
-    for (uint32_t j = 0; j < 4; ++j)
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            const uint32_t k = 8 * j + 2 * i;
-            const uint32_t lo = k < n ? ((const uint16_t*)p)[k] : 0, hi = k + 1 < n ? ((const uint16_t*)p)[k + 1] : 0;
-            o.v[0][j][i] = lo | hi << 16;
+        for (uint32_t i = 0; i < kVecs; ++i) {
+            const uint8_t* q = p + 16 * i;
+            if constexpr (KIND == kRowsF32) v[i] = *(const Any<float>::vec16*)q;
+            else if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
+            else v[i] = *(const Any<uint8_t>::vec16*)q;
         }
+        if constexpr (KIND == kRowsMx8) scale = *scale_at;
+    }
+
+    // The last k tile, of `left` values from k block 0 on: zeros behind them.
+    __device__ __forceinline__ void load_last(const uint8_t* p, const uint8_t* scale_at, uint32_t lq, uint32_t left)
+    {
+        constexpr uint32_t es = row_size(KIND), kEach = 16 / es;                // values of a vector
+#pragma unroll
+        for (uint32_t i = 0; i < kVecs; ++i) {
+            const uint32_t first = lq * 32 + kEach * i;     // ... its first one
+            const uint8_t* q = p + 16 * i;
+            v[i] = u32x4{0, 0, 0, 0};
+            if (first + kEach <= left) {
+                if constexpr (KIND == kRowsF32) v[i] = *(const Any<float>::vec16*)q;
+                else if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
+                else v[i] = *(const Any<uint8_t>::vec16*)q;
+            } else if (first < left) {
+#pragma unroll
+                for (uint32_t e = 0; e < kEach; ++e)
+                    if (first + e < left) {
+                        if constexpr (es == 4) v[i][e] = ((const uint32_t*)q)[e];
+                        else if constexpr (es == 2) v[i][e / 2] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e % 2));
+                        else v[i][e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
+                    }
+            }
+        }
+        if constexpr (KIND == kRowsMx8) scale = lq * 32 < left ? *scale_at : 127;
+    }
+};
+
+// ... and as operands of four 16x16x32 instructions (times three for fp32).
+template <Kind KIND> struct RowOperand {
+    static constexpr int kParts = KIND == kRowsF32 ? 3 : 1;
+    u32x4 v[kParts][4];
+    __device__ __forceinline__ explicit RowOperand(const RawRow<KIND>& r)
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (KIND == kRowsBf16) v[0][j] = r.v[j];
+            else if constexpr (KIND == kRowsF32) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f32x4 f = __builtin_bit_cast(f32x4, r.v[2 * j + h]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t lo[3], hi[3];
+                        split3(f[2 * i], lo); split3(f[2 * i + 1], hi);
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) v[q][j][2 * h + i] = lo[q] >> 16 | hi[q];
+                    }
+                }
+            } else if constexpr (KIND == kRowsMx8) {
+                // 2^(scale - 127); the smallest is subnormal, the largest byte is NaN
+                const float s = __builtin_bit_cast(float, r.scale == 0xff ? 0x7fc00000u : r.scale ? r.scale << 23 : 0x00400000u);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t w = r.v[j / 2][2 * (j % 2) + i];
+                    v[0][j][2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false));
+                    v[0][j][2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true));
+                }
+            }
+        }
+    }
+};
+
+// A lane's 32 weights and their scale.
+struct RawWeights { u32x4 codes; uint32_t scale; };
+__device__ __forceinline__ RawWeights load_weights(const uint8_t* tile, uint32_t lane)
+{
+    return RawWeights{*(const u32x4*)(tile + lane * 16), tile[kTile4Codes + lane]};
 }
-__device__ __forceinline__ void load_operand(Operand<RowsF32>& o, const Linear4Args& a, uint64_t row, uint32_t at, uint32_t width, bool there)
+__device__ __forceinline__ void weights_of(const RawWeights& r, u32x4 (&w)[4])
 {
-    const float* p = (const float*)a.x + row * a.x_stride + at;
-    const uint32_t n = there && at < width ? (width - at < 32 ? width - at : 32) : 0;
+    const float s = __builtin_bit_cast(float, r.scale << 23);
 #pragma unroll
-    for (uint32_t j = 0; j < 4; ++j) {
-        float f[8];
-        if (n == 32) load8(p + 8 * j, f); else load_some(p + 8 * j, n > 8 * j ? n - 8 * j : 0, f);
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) {
-            uint32_t lo[3], hi[3];
-            split3(f[2 * i], lo); split3(f[2 * i + 1], hi);
-#pragma unroll
-            for (int q = 0; q < 3; ++q) o.v[q][j][i] = lo[q] >> 16 | hi[q];
-        }
-    }
-}
-__device__ __forceinline__ void load_operand(Operand<RowsMx8>& o, const Linear4Args& a, uint64_t row, uint32_t at, uint32_t width, bool there)
-{
-    const uint8_t* p = (const uint8_t*)a.x + row * a.x_stride + at;
-    const uint32_t n = there && at < width ? (width - at < 32 ? width - at : 32) : 0;
-    uint32_t w[8];
-    if (n == 32) {
-        const u32x4 w0 = *(const Any<uint8_t>::vec16*)p, w1 = *(const Any<uint8_t>::vec16*)(p + 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { w[i] = w0[i]; w[4 + i] = w1[i]; }
-    } else {
-#pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            w[i] = 0;
-#pragma unroll
-            for (uint32_t e = 0; e < 4; ++e) if (4 * i + e < n) w[i] |= (uint32_t)p[4 * i + e] << (8 * e);
-        }
-    }
-    const uint32_t sb = n ? a.x_scales[row * a.x_scales_stride + at / MT_MX_BLOCK] : 127;
-    // 2^(sb - 127); the smallest is subnormal, the largest byte is NaN
-    const float scale = __builtin_bit_cast(float, sb == 0xff ? 0x7fc00000u : sb ? sb << 23 : 0x00400000u);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        o.v[0][i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, false));
-        o.v[0][i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[i], scale, true));
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t c = r.codes[j];
+        w[j][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+        w[j][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+        w[j][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+        w[j][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
     }
 }
 
-// A lane's 32 weights, scaled, as operands of four matrix instructions.
-__device__ __forceinline__ void weights_of(const u32x4& codes, uint32_t scale_byte, u32x4 (&w)[4])
-{
-    const float s = __builtin_bit_cast(float, scale_byte << 23);
+// One k tile: NT tiles of 16 outputs, RT tiles of 16 rows.
+template <Kind KIND, int RT, int NT> struct Step {
+    RawWeights w[NT];
+    RawRow<KIND> x[RT];
+
+    __device__ __forceinline__ void multiply(f32x4 (&acc)[NT][RT]) const
+    {
+                    u32x4 wv[NT][4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        w[j][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[j], s, 0));
-        w[j][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[j], s, 1));
-        w[j][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[j], s, 2));
-        w[j][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[j], s, 3));
+                    for (int n = 0; n < NT; ++n) weights_of(w[n], wv[n]);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        const RowOperand<KIND> o(x[r]);
+#pragma unroll
+                        for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    acc[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[n][j]), __builtin_bit_cast(bf16x8, o.v[p][j]), acc[n][r], 0, 0, 0);
+                    }
     }
-}
+};
 
 // NaN stays NaN in both.
 __device__ __forceinline__ float activate4(float z, uint32_t act)
@@ -116,82 +161,146 @@ __device__ __forceinline__ float activate4(float z, uint32_t act)
     return z;
 }
 
-__device__ __forceinline__ void store4(__bf16* p, const f32x4& v)
-{
-    *(Any<__bf16>::vec8*)p = Any<__bf16>::vec8{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-}
+__device__ __forceinline__ void store4(__bf16* p, const f32x4& v) { *(Any<__bf16>::vec8*)p = Any<__bf16>::vec8{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *(Any<float>::vec16*)p = __builtin_bit_cast(u32x4, v); }
 
-// WK waves share the k tiles of 16 outputs times 16 rows and add their sums up through LDS.
-template <typename X, typename Y, int WK>
-__global__ void __launch_bounds__(WK * 64) linear4_kernel(Linear4Args a)
+template <typename Y>
+__device__ __forceinline__ void store_outputs(const Linear4Args& a, uint64_t row, uint32_t n0, uint32_t N, const f32x4& v)
+{
+    Y* y = (Y*)a.y + row * a.y_stride + n0;
+    if (n0 + 4 <= N) store4(y, v);
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) if (n0 + i < N) y[i] = (Y)v[i];
+}
+
+constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles and add their sums up through LDS
+
+// A workgroup serves 16 NT outputs of 16 RT rows of a group; a wave asks for DEPTH k tiles at a time, the next ones before it multiplies.
+template <Kind KIND, int RT, int NT, int DEPTH>
+__global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     // the group is the last one that starts at or before this workgroup
-    const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
-    const uint32_t gi = __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
+    uint32_t gi = 0;
+    if (a.n_groups > 1) {
+        const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
+        gi = __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
+    }
     const Group4& g = a.groups[gi];
     const uint32_t N = g.N, K = g.K;
-    const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K);
+    const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_slabs = ceil_div(n_tiles, NT);
     const uint32_t local = blockIdx.x - g.wg_base;
-    const uint32_t tile = local % n_tiles, row_tile = local / n_tiles;
+    const uint32_t slab = local % n_slabs, first_row = local / n_slabs * (16 * RT);
     const uint32_t li = lane & 15, lq = lane >> 4;
-    const uint32_t in_group = row_tile * 16 + li;
-    const bool there = in_group < g.n_rows;
-    const uint64_t row = (uint64_t)g.row0 + in_group;
-    const uint8_t* w = a.arena + g.off + (uint64_t)tile * k_tiles * kTile4Bytes;
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t kt = wave; kt < k_tiles; kt += WK) {
-        const u32x4 codes = *(const u32x4*)(w + (uint64_t)kt * kTile4Bytes + lane * 16);
-        const uint32_t sb = w[(uint64_t)kt * kTile4Bytes + kTile4Codes + lane];
-        Operand<X> x;
-        load_operand(x, a, row, kt * kTile4K + lq * 32, K, there);
-        u32x4 wv[4];
-        weights_of(codes, sb, wv);
+    const uint8_t* w[NT];
 #pragma unroll
-        for (int p = Operand<X>::kParts - 1; p >= 0; --p)
+    for (int n = 0; n < NT; ++n) w[n] = a.arena + g.off + (uint64_t)min(slab * NT + n, n_tiles - 1) * k_tiles * kTile4Bytes;
+    const uint8_t *x[RT], *xs[RT];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[j]), __builtin_bit_cast(bf16x8, x.v[p][j]), acc, 0, 0, 0);
+    for (int r = 0; r < RT; ++r) {
+        const uint64_t row = (uint64_t)g.row0 + min(first_row + 16 * r + li, g.n_rows - 1);
+        x[r] = (const uint8_t*)a.x + row * a.x_stride * row_size(KIND) + lq * (32 * row_size(KIND));
+        xs[r] = a.x_scales + row * a.x_scales_stride + lq;
     }
-    __shared__ f32x4 part[WK][64];
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave != 0) return;
+    f32x4 acc[NT][RT];
 #pragma unroll
-    for (int i = 1; i < WK; ++i) acc += part[i][lane];
-    // lane l: row l % 16, outputs 4 (l / 16) .. + 3 of the tile
-    const uint32_t n0 = tile * kTile4Rows + 4 * lq;
-    if (!there || n0 >= N) return;
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[n][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    // whole k tiles: this wave's are wave, wave + 4, ...
+    const uint32_t whole = K / kTile4K;
+    Step<KIND, RT, NT> at[2][DEPTH];
+    const auto ask = [&](Step<KIND, RT, NT> (&to)[DEPTH], uint32_t kt) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const uint32_t t = min(kt + d * kWaves4, whole - 1);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) to[d].w[n] = load_weights(w[n] + (uint64_t)t * kTile4Bytes, lane);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) to[d].x[r].load(x[r] + t * (kTile4K * row_size(KIND)), xs[r] + t * 4);
+        }
+    };
+    const auto use = [&](const Step<KIND, RT, NT> (&of)[DEPTH], uint32_t kt) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) if (d == 0 || kt + d * kWaves4 < whole) of[d].multiply(acc);
+    };
+    constexpr uint32_t kStride = DEPTH * kWaves4;
+    if (wave < whole) {
+        uint32_t kt = wave;
+        ask(at[0], kt);
+        while (true) {
+            if (kt + kStride < whole) ask(at[1], kt + kStride);
+            use(at[0], kt);
+            kt += kStride;
+            if (kt >= whole) break;
+            if (kt + kStride < whole) ask(at[0], kt + kStride);
+            use(at[1], kt);
+            kt += kStride;
+            if (kt >= whole) break;
+        }
+    }
+    if (whole < k_tiles && whole % kWaves4 == wave) {           // the last one, where it is not whole
+        Step<KIND, RT, NT> last;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) last.w[n] = load_weights(w[n] + (uint64_t)whole * kTile4Bytes, lane);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) last.x[r].load_last(x[r] + (uint64_t)whole * (kTile4K * row_size(KIND)), xs[r] + whole * 4, lq, K - whole * kTile4K);
+        last.multiply(acc);
+    }
+
+    // tile t of the NT x RT is finished by wave t % 4
+    __shared__ f32x4 part[kWaves4][NT * RT][64];
+#pragma unroll
+    for (int t = 0; t < NT * RT; ++t) if (t % kWaves4 != (int)wave) part[wave][t][lane] = acc[t / RT][t % RT];
+    __syncthreads();
     const float* bias = g.has_bias ? (const float*)(a.arena + g.off + matrix4_tiles_bytes(N, K)) : nullptr;
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) acc[i] = activate4(acc[i] + (bias && n0 + i < N ? bias[n0 + i] : 0.0f), a.act);
-    Y* y = (Y*)a.y + row * a.y_stride + n0;
-    if (n0 + 4 <= N) store4(y, acc);
-    else
+    for (int t = 0; t < NT * RT; ++t) {
+        if (t % kWaves4 != (int)wave) continue;
+        f32x4 v = acc[t / RT][t % RT];
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) if (n0 + i < N) y[i] = (Y)acc[i];
+        for (int o = 1; o < kWaves4; ++o) v += part[(wave + o) % kWaves4][t][lane];
+        // lane l: row l % 16, outputs 4 (l / 16) .. + 3 of the tile
+        const uint32_t n0 = (slab * NT + t / RT) * kTile4Rows + 4 * lq, in_group = first_row + 16 * (t % RT) + li;
+        if (in_group >= g.n_rows || n0 >= N) continue;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) v[i] = activate4(v[i] + (bias && n0 + i < N ? bias[n0 + i] : 0.0f), a.act);
+        if (a.y_bf16) store_outputs<__bf16>(a, (uint64_t)g.row0 + in_group, n0, N, v);
+        else store_outputs<float>(a, (uint64_t)g.row0 + in_group, n0, N, v);
+    }
 }
 
-template <typename X, typename Y>
-hipError_t go(const Linear4Args& a, Linear4Shape, uint32_t grid, hipStream_t s)
+template <Kind KIND, int RT, int NT, int DEPTH>
+hipError_t go(const Linear4Args& a, uint32_t grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((linear4_kernel<X, Y, 4>), dim3(grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((linear4_kernel<KIND, RT, NT, DEPTH>), dim3(grid), dim3(kWaves4 * 64), 0, s, a);
     return hipGetLastError();
+}
+
+template <Kind KIND>
+hipError_t choose(const Linear4Args& a, Linear4Shape shape, uint32_t grid, hipStream_t s)
+{
+    if (shape.rt == 1) return shape.nt == 1 ? go<KIND, 1, 1, KIND == kRowsF32 ? 1 : 4>(a, grid, s) : go<KIND, 1, 4, 1>(a, grid, s);
+    if constexpr (KIND == kRowsF32) return go<KIND, 2, 4, 1>(a, grid, s);
+    else return shape.rt == 2 ? go<KIND, 2, 4, 1>(a, grid, s) : go<KIND, 4, 4, 1>(a, grid, s);
 }
 
 }  // namespace
 
-Linear4Shape linear4_shape(uint64_t, uint32_t, uint32_t, uint32_t) { return Linear4Shape{1, 1, 4}; }
-
-hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t y_dtype, uint32_t grid, hipStream_t s)
+Linear4Shape linear4_shape(uint64_t tiles, uint32_t, uint32_t most_rows, uint32_t n_cus, uint32_t x_dtype)
 {
-    if (y_dtype == MT_BF16) {
-        if (x_dtype == MT_MX8) return go<RowsMx8, __bf16>(a, shape, grid, s);
-        return x_dtype == MT_BF16 ? go<RowsBf16, __bf16>(a, shape, grid, s) : go<RowsF32, __bf16>(a, shape, grid, s);
-    }
-    if (x_dtype == MT_MX8) return go<RowsMx8, float>(a, shape, grid, s);
-    return x_dtype == MT_BF16 ? go<RowsBf16, float>(a, shape, grid, s) : go<RowsF32, float>(a, shape, grid, s);
+    Linear4Shape s;
+    s.rt = most_rows <= 16 ? 1 : most_rows <= 32 || x_dtype == MT_F32 ? 2 : 4;
+    s.nt = s.rt > 1 || tiles >= 16 * (uint64_t)n_cus ? 4 : 1;
+    return s;
+}
+
+hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s)
+{
+    if (x_dtype == MT_MX8) return choose<kRowsMx8>(a, shape, grid, s);
+    return x_dtype == MT_BF16 ? choose<kRowsBf16>(a, shape, grid, s) : choose<kRowsF32>(a, shape, grid, s);
 }
 
 }  // namespace mt

@@ -338,7 +338,7 @@ struct Linear4Args {
     const uint8_t* arena;
     const void* x; const uint8_t* x_scales; void* y;
     uint64_t x_stride, x_scales_stride, y_stride;
-    uint32_t act, n_groups;
+    uint32_t act, n_groups, y_bf16;
     Group4 groups[kGroups4];
 };
 static_assert(sizeof(Linear4Args) <= 4096, "kernel arguments");
@@ -348,10 +348,9 @@ struct ScoreArgs {
     uint32_t parts, part_len;        // workgroups that share a row, and classes of one of them
 };
 hipError_t launch_norm(const mt_norm_args& a, hipStream_t s);
-// How linear4's launches are shaped, for groups of one shape class; see launch_linear4.
-struct Linear4Shape { uint32_t rt, nt, wk; };
-Linear4Shape linear4_shape(uint64_t tiles, uint32_t k_tiles, uint32_t most_rows, uint32_t n_cus);
-hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t y_dtype, uint32_t grid, hipStream_t s);
+struct Linear4Shape { uint32_t rt, nt; };      // tiles of 16 rows and of 16 outputs that a workgroup serves
+Linear4Shape linear4_shape(uint64_t tiles, uint32_t k_tiles, uint32_t most_rows, uint32_t n_cus, uint32_t x_dtype);
+hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s);
 void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len);
 uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top);
 hipError_t launch_score(const ScoreArgs& a, hipStream_t s);
