@@ -29,6 +29,15 @@ __device__ __forceinline__ void split3(float x, uint32_t (&part)[3])
     if (special) { part[0] |= (b & 0xffffu) ? 0x400000u : 0u; part[1] = part[2] = 0; }
 }
 
+// 2^(byte - 127); the smallest is subnormal, the largest byte is NaN.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte == 0xff ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u); }
+// Eight 8-bit values, scaled, as bf16.
+__device__ __forceinline__ u32x4 eight_of(uint32_t lo, uint32_t hi, float s)
+{
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true))};
+}
+
 // A lane's 32 values of a row as they come from memory.
 template <Kind KIND> struct RawRow {
     static constexpr uint32_t kVecs = row_size(KIND) * 2;      // of 16 bytes
@@ -97,14 +106,7 @@ template <Kind KIND> struct RowOperand {
                     }
                 }
             } else if constexpr (KIND == kRowsMx8) {
-                // 2^(scale - 127); the smallest is subnormal, the largest byte is NaN
-                const float s = __builtin_bit_cast(float, r.scale == 0xff ? 0x7fc00000u : r.scale ? r.scale << 23 : 0x00400000u);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const uint32_t w = r.v[j / 2][2 * (j % 2) + i];
-                    v[0][j][2 * i] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, false));
-                    v[0][j][2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, s, true));
-                }
+                v[0][j] = eight_of(r.v[j / 2][2 * (j % 2)], r.v[j / 2][2 * (j % 2) + 1], scale_of(r.scale));
             }
         }
     }
@@ -116,17 +118,18 @@ __device__ __forceinline__ RawWeights load_weights(const uint8_t* tile, uint32_t
 {
     return RawWeights{*(const u32x4*)(tile + lane * 16), tile[kTile4Codes + lane]};
 }
-__device__ __forceinline__ void weights_of(const RawWeights& r, u32x4 (&w)[4])
+// ... the j-th eight of them, scaled, as an operand.
+__device__ __forceinline__ u32x4 weights_of(const RawWeights& r, int j)
 {
     const float s = __builtin_bit_cast(float, r.scale << 23);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint32_t c = r.codes[j];
-        w[j][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
-        w[j][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
-        w[j][2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
-        w[j][3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
-    }
+    const uint32_t c = r.codes[j];
+    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1)),
+                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3))};
+}
+
+__device__ __forceinline__ f32x4 mfma(const u32x4& w, const u32x4& x, const f32x4& acc)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
 }
 
 // One k tile: NT tiles of 16 outputs, RT tiles of 16 rows.
@@ -136,20 +139,21 @@ template <Kind KIND, int RT, int NT> struct Step {
 
     __device__ __forceinline__ void multiply(f32x4 (&acc)[NT][RT]) const
     {
-                    u32x4 wv[NT][4];
+        u32x4 wv[NT][4];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) weights_of(w[n], wv[n]);
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) {
-                        const RowOperand<KIND> o(x[r]);
+            for (int j = 0; j < 4; ++j) wv[n][j] = weights_of(w[n], j);
 #pragma unroll
-                        for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
+        for (int r = 0; r < RT; ++r) {
+            const RowOperand<KIND> o(x[r]);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
+            for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
 #pragma unroll
-                                for (int n = 0; n < NT; ++n)
-                                    acc[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wv[n][j]), __builtin_bit_cast(bf16x8, o.v[p][j]), acc[n][r], 0, 0, 0);
-                    }
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) acc[n][r] = mfma(wv[n][j], o.v[p][j], acc[n][r]);
+        }
     }
 };
 
@@ -172,6 +176,17 @@ __device__ __forceinline__ void store_outputs(const Linear4Args& a, uint64_t row
     else
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) if (n0 + i < N) y[i] = (Y)v[i];
+}
+
+// Four outputs of a row of the group: bias, activation, store.
+__device__ __forceinline__ void finish_tile(const Linear4Args& a, const Group4& g, uint32_t n0, uint32_t in_group, f32x4 v)
+{
+    if (in_group >= g.n_rows || n0 >= g.N) return;
+    const float* bias = g.has_bias ? (const float*)(a.arena + g.off + matrix4_tiles_bytes(g.N, g.K)) : nullptr;
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) v[i] = activate4(v[i] + (bias && n0 + i < g.N ? bias[n0 + i] : 0.0f), a.act);
+    if (a.y_bf16) store_outputs<__bf16>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
+    else store_outputs<float>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
 }
 
 constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles and add their sums up through LDS
@@ -255,22 +270,168 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 #pragma unroll
     for (int t = 0; t < NT * RT; ++t) if (t % kWaves4 != (int)wave) part[wave][t][lane] = acc[t / RT][t % RT];
     __syncthreads();
-    const float* bias = g.has_bias ? (const float*)(a.arena + g.off + matrix4_tiles_bytes(N, K)) : nullptr;
 #pragma unroll
     for (int t = 0; t < NT * RT; ++t) {
         if (t % kWaves4 != (int)wave) continue;
         f32x4 v = acc[t / RT][t % RT];
 #pragma unroll
         for (int o = 1; o < kWaves4; ++o) v += part[(wave + o) % kWaves4][t][lane];
-        // lane l: row l % 16, outputs 4 (l / 16) .. + 3 of the tile
-        const uint32_t n0 = (slab * NT + t / RT) * kTile4Rows + 4 * lq, in_group = first_row + 16 * (t % RT) + li;
-        if (in_group >= g.n_rows || n0 >= N) continue;
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) v[i] = activate4(v[i] + (bias && n0 + i < N ? bias[n0 + i] : 0.0f), a.act);
-        if (a.y_bf16) store_outputs<__bf16>(a, (uint64_t)g.row0 + in_group, n0, N, v);
-        else store_outputs<float>(a, (uint64_t)g.row0 + in_group, n0, N, v);
+        finish_tile(a, g, (slab * NT + t / RT) * kTile4Rows + 4 * lq, first_row + 16 * (t % RT) + li, v);
     }
 }
+
+// ---- many rows: rows through LDS ----------------------------------------------------------------
+// 16 RT rows and 128 outputs to a workgroup of eight waves: 64 outputs (slab) x a quarter of the k tiles to each.  The two waves of a quarter fetch its rows
+// together, 16 bytes a lane along the rows (read in place by operands, a load would touch 64 lines; 512 rows through 4096 x 4096 took 44.6 us that way), and
+// put them into LDS as bf16 operands: chunk c (eight values) of row i at slot i ^ c of its sixteen, so that neither the stores along a row nor the loads
+// down the rows meet in a bank.  Two buffers, so one barrier for a k tile.  The weights go from memory to registers two k tiles ahead.
+constexpr int kSlabs = 2, kQuarters = 4, kNt = 4;
+
+template <Kind KIND, int RT> struct RowFetch {
+    static constexpr uint32_t kPer = 16 / row_size(KIND), kAcross = kTile4K / kPer;         // values of a load; loads along a row
+    static constexpr uint32_t kRowsAtOnce = 128 / kAcross, kPasses = 16 * RT / kRowsAtOnce;
+    const uint8_t* p[kPasses];
+    const uint8_t* ps[KIND == kRowsMx8 ? kPasses : 1];
+    u32x4 v[kPasses];
+    uint32_t scale[KIND == kRowsMx8 ? kPasses : 1];
+    uint32_t u, row0;              // which load along the row, and row, this thread starts with
+
+    __device__ __forceinline__ RowFetch(const Linear4Args& a, const Group4& g, uint32_t first_row, uint32_t t) : u(t % kAcross), row0(t / kAcross)
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kPasses; ++i) {
+            const uint64_t row = (uint64_t)g.row0 + min(first_row + row0 + i * kRowsAtOnce, g.n_rows - 1);
+            p[i] = (const uint8_t*)a.x + row * a.x_stride * row_size(KIND) + u * 16;
+            if constexpr (KIND == kRowsMx8) ps[i] = a.x_scales + row * a.x_scales_stride + u / 2;
+        }
+    }
+    __device__ __forceinline__ void ask(uint32_t kt, uint32_t K)
+    {
+        const uint32_t at = kt * kTile4K, left = K - at;
+        if (left >= kTile4K) {
+#pragma unroll
+            for (uint32_t i = 0; i < kPasses; ++i) {
+                const uint8_t* q = p[i] + at * row_size(KIND);
+                if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
+                else { v[i] = *(const Any<uint8_t>::vec16*)q; scale[i] = ps[i][at / MT_MX_BLOCK]; }
+            }
+        } else {                   // the last k tile, not whole: zeros behind the row's end
+#pragma unroll
+            for (uint32_t i = 0; i < kPasses; ++i) {
+                const uint8_t* q = p[i] + at * row_size(KIND);
+                v[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+                for (uint32_t e = 0; e < kPer; ++e)
+                    if (u * kPer + e < left) {
+                        if constexpr (KIND == kRowsBf16) v[i][e / 2] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e % 2));
+                        else v[i][e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
+                    }
+                if constexpr (KIND == kRowsMx8) scale[i] = u * kPer < left ? ps[i][at / MT_MX_BLOCK] : 127;
+            }
+        }
+    }
+    static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t c)      // in 16 bytes
+    {
+        return ((row / 16 * 4 + c % 4) * 4 + c / 4) * 16 + (row % 16 ^ c);
+    }
+    __device__ __forceinline__ void put(u32x4* to) const
+    {
+#pragma unroll
+        for (uint32_t i = 0; i < kPasses; ++i) {
+            const uint32_t row = row0 + i * kRowsAtOnce;
+            if constexpr (KIND == kRowsBf16) to[place(row, u)] = v[i];
+            else {
+                const float s = scale_of(scale[i]);
+                to[place(row, 2 * u)] = eight_of(v[i][0], v[i][1], s);
+                to[place(row, 2 * u + 1)] = eight_of(v[i][2], v[i][3], s);
+            }
+        }
+    }
+};
+
+template <Kind KIND, int RT>
+__global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
+{
+    extern __shared__ __attribute__((aligned(16))) u32x4 lds[];
+    constexpr uint32_t kTileVecs = 16 * RT * 16;              // a k tile of the rows, in 16 bytes
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t quarter = wave / kSlabs, li = lane & 15, lq = lane >> 4;
+    uint32_t gi = 0;
+    if (a.n_groups > 1) {
+        const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
+        gi = __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
+    }
+    const Group4& g = a.groups[gi];
+    const uint32_t N = g.N, K = g.K;
+    const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_wide = ceil_div(n_tiles, kNt * kSlabs), chunks = ceil_div(g.n_rows, 16 * RT);
+    // workgroups eight apart share an XCD: they take the same outputs of one chunk of rows after the other
+    const uint32_t local = blockIdx.x - g.wg_base, in_eights = n_wide / 8 * 8 * chunks;
+    uint32_t wide, chunk;
+    if (local < in_eights) { wide = local / (8 * chunks) * 8 + local % 8; chunk = local / 8 % chunks; }
+    else { const uint32_t rest = local - in_eights, n = n_wide % 8; wide = n_wide - n + rest % n; chunk = rest / n; }
+    const uint32_t slab = wide * kSlabs + wave % kSlabs, first_row = chunk * (16 * RT);
+    const uint8_t* w[kNt];
+#pragma unroll
+    for (int n = 0; n < kNt; ++n) w[n] = a.arena + g.off + (uint64_t)min(slab * kNt + n, n_tiles - 1) * k_tiles * kTile4Bytes;
+    RowFetch<KIND, RT> x(a, g, first_row, threadIdx.x % (64 * kSlabs));
+    f32x4 acc[kNt][RT];
+#pragma unroll
+    for (int n = 0; n < kNt; ++n)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[n][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    RawWeights ws[2][kNt];
+    const auto ask_weights = [&](RawWeights (&to)[kNt], uint32_t kt) {
+        if (kt < k_tiles) {
+#pragma unroll
+            for (int n = 0; n < kNt; ++n) to[n] = load_weights(w[n] + (uint64_t)kt * kTile4Bytes, lane);
+        }
+    };
+    ask_weights(ws[0], quarter);
+    if (quarter < k_tiles) x.ask(quarter, K);
+    ask_weights(ws[1], quarter + kQuarters);
+    const auto step = [&](RawWeights (&wt)[kNt], uint32_t kt, uint32_t buffer) {
+        u32x4* tile = lds + (quarter * 2 + buffer) * kTileVecs;
+        if (kt < k_tiles) x.put(tile);
+        if (kt + kQuarters < k_tiles) x.ask(kt + kQuarters, K);
+        lds_barrier();
+        if (kt < k_tiles) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u32x4 o[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) o[r] = tile[((r * 4 + j) * 4 + lq) * 16 + (li ^ (lq * 4 + j))];
+#pragma unroll
+                for (int n = 0; n < kNt; ++n) {
+                    const u32x4 wv = weights_of(wt[n], j);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[n][r] = mfma(wv, o[r], acc[n][r]);
+                }
+            }
+        }
+        ask_weights(wt, kt + 2 * kQuarters);
+    };
+    for (uint32_t kt = quarter, base = 0; base < k_tiles; base += 2 * kQuarters, kt += 2 * kQuarters) {
+        step(ws[0], kt, 0);
+        if (base + kQuarters < k_tiles) step(ws[1], kt + kQuarters, 1);
+    }
+    // a wave finishes RT of its slab's tiles, with the sums of the other quarters
+    __syncthreads();
+    f32x4* part = (f32x4*)lds;
+    const auto at = [&](uint32_t q, uint32_t t) { return ((q * kSlabs + wave % kSlabs) * (kNt * RT) + t) * 64 + lane; };
+#pragma unroll
+    for (int t = 0; t < kNt * RT; ++t) if (t % kQuarters != (int)quarter) part[at(quarter, t)] = acc[t / RT][t % RT];
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < kNt * RT; ++t) {
+        if (t % kQuarters != (int)quarter) continue;
+        f32x4 v = acc[t / RT][t % RT];
+#pragma unroll
+        for (int o = 1; o < kQuarters; ++o) v += part[at((quarter + o) % kQuarters, t)];
+        finish_tile(a, g, (slab * kNt + t / RT) * kTile4Rows + 4 * lq, first_row + 16 * (t % RT) + li, v);
+    }
+}
+template <int RT> constexpr uint32_t rows_lds() { return kQuarters * kSlabs * (kNt * RT) * 1024; }      // the sums at the end; both buffers of rows take no more
+static_assert(rows_lds<4>() >= kQuarters * 2 * 64 * 256 && rows_lds<4>() <= 160 * 1024, "LDS");
 
 template <Kind KIND, int RT, int NT, int DEPTH>
 hipError_t go(const Linear4Args& a, uint32_t grid, hipStream_t s)
@@ -279,13 +440,23 @@ hipError_t go(const Linear4Args& a, uint32_t grid, hipStream_t s)
     return hipGetLastError();
 }
 
+template <Kind KIND, int RT>
+hipError_t go_rows(const Linear4Args& a, uint32_t grid, hipStream_t s)
+{
+    hipLaunchKernelGGL((linear4_rows_kernel<KIND, RT>), dim3(grid), dim3(512), rows_lds<RT>(), s, a);
+    return hipGetLastError();
+}
+
 template <Kind KIND>
 hipError_t choose(const Linear4Args& a, Linear4Shape shape, uint32_t grid, hipStream_t s)
 {
     if (shape.rt == 1) return shape.nt == 1 ? go<KIND, 1, 1, KIND == kRowsF32 ? 1 : 4>(a, grid, s) : go<KIND, 1, 4, 1>(a, grid, s);
     if constexpr (KIND == kRowsF32) return go<KIND, 2, 4, 1>(a, grid, s);
-    else return shape.rt == 2 ? go<KIND, 2, 4, 1>(a, grid, s) : go<KIND, 4, 4, 1>(a, grid, s);
+    else return shape.rt == 2 ? go_rows<KIND, 2>(a, grid, s) : go_rows<KIND, 4>(a, grid, s);
 }
+
+template <Kind KIND, int RT>
+hipError_t prepare_rows() { return hipFuncSetAttribute((const void*)linear4_rows_kernel<KIND, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, rows_lds<RT>()); }
 
 }  // namespace
 
@@ -293,8 +464,16 @@ Linear4Shape linear4_shape(uint64_t tiles, uint32_t, uint32_t most_rows, uint32_
 {
     Linear4Shape s;
     s.rt = most_rows <= 16 ? 1 : most_rows <= 32 || x_dtype == MT_F32 ? 2 : 4;
-    s.nt = s.rt > 1 || tiles >= 16 * (uint64_t)n_cus ? 4 : 1;
+    s.nt = s.rt > 1 ? (x_dtype == MT_F32 ? 4 : kNt * kSlabs) : tiles >= 16 * (uint64_t)n_cus ? 4 : 1;
     return s;
+}
+
+hipError_t prepare_linear4()
+{
+    hipError_t e = prepare_rows<kRowsBf16, 2>();
+    if (e == hipSuccess) e = prepare_rows<kRowsBf16, 4>();
+    if (e == hipSuccess) e = prepare_rows<kRowsMx8, 2>();
+    return e == hipSuccess ? prepare_rows<kRowsMx8, 4>() : e;
 }
 
 hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s)
