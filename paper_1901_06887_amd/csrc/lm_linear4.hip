@@ -305,29 +305,29 @@ template <Kind KIND, int RT> struct RowFetch {
             if constexpr (KIND == kRowsMx8) ps[i] = a.x_scales + row * a.x_scales_stride + u / 2;
         }
     }
-    __device__ __forceinline__ void ask(uint32_t kt, uint32_t K)
+    __device__ __forceinline__ void ask(uint32_t kt)
     {
-        const uint32_t at = kt * kTile4K, left = K - at;
-        if (left >= kTile4K) {
 #pragma unroll
-            for (uint32_t i = 0; i < kPasses; ++i) {
-                const uint8_t* q = p[i] + at * row_size(KIND);
-                if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
-                else { v[i] = *(const Any<uint8_t>::vec16*)q; scale[i] = ps[i][at / MT_MX_BLOCK]; }
-            }
-        } else {                   // the last k tile, not whole: zeros behind the row's end
+        for (uint32_t i = 0; i < kPasses; ++i) {
+            const uint8_t* q = p[i] + kt * (kTile4K * row_size(KIND));
+            if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
+            else { v[i] = *(const Any<uint8_t>::vec16*)q; scale[i] = ps[i][kt * (kTile4K / MT_MX_BLOCK)]; }
+        }
+    }
+    // The last k tile where it is not whole, `left` values long: zeros behind them.
+    __device__ __forceinline__ void ask_last(uint32_t kt, uint32_t left)
+    {
 #pragma unroll
-            for (uint32_t i = 0; i < kPasses; ++i) {
-                const uint8_t* q = p[i] + at * row_size(KIND);
-                v[i] = u32x4{0, 0, 0, 0};
+        for (uint32_t i = 0; i < kPasses; ++i) {
+            const uint8_t* q = p[i] + kt * (kTile4K * row_size(KIND));
+            v[i] = u32x4{0, 0, 0, 0};
 #pragma unroll
-                for (uint32_t e = 0; e < kPer; ++e)
-                    if (u * kPer + e < left) {
-                        if constexpr (KIND == kRowsBf16) v[i][e / 2] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e % 2));
-                        else v[i][e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
-                    }
-                if constexpr (KIND == kRowsMx8) scale[i] = u * kPer < left ? ps[i][at / MT_MX_BLOCK] : 127;
-            }
+            for (uint32_t e = 0; e < kPer; ++e)
+                if (u * kPer + e < left) {
+                    if constexpr (KIND == kRowsBf16) v[i][e / 2] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e % 2));
+                    else v[i][e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
+                }
+            if constexpr (KIND == kRowsMx8) scale[i] = u * kPer < left ? ps[i][kt * (kTile4K / MT_MX_BLOCK)] : 127;
         }
     }
     static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t c)      // in 16 bytes
@@ -379,40 +379,58 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
     for (int n = 0; n < kNt; ++n)
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[n][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    RawWeights ws[2][kNt];
     const auto ask_weights = [&](RawWeights (&to)[kNt], uint32_t kt) {
-        if (kt < k_tiles) {
 #pragma unroll
-            for (int n = 0; n < kNt; ++n) to[n] = load_weights(w[n] + (uint64_t)kt * kTile4Bytes, lane);
-        }
+        for (int n = 0; n < kNt; ++n) to[n] = load_weights(w[n] + (uint64_t)kt * kTile4Bytes, lane);
     };
-    ask_weights(ws[0], quarter);
-    if (quarter < k_tiles) x.ask(quarter, K);
-    ask_weights(ws[1], quarter + kQuarters);
-    const auto step = [&](RawWeights (&wt)[kNt], uint32_t kt, uint32_t buffer) {
-        u32x4* tile = lds + (quarter * 2 + buffer) * kTileVecs;
-        if (kt < k_tiles) x.put(tile);
-        if (kt + kQuarters < k_tiles) x.ask(kt + kQuarters, K);
-        lds_barrier();
-        if (kt < k_tiles) {
+    const auto multiply = [&](const RawWeights (&wt)[kNt], const u32x4* tile) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                u32x4 o[RT];
+        for (int j = 0; j < 4; ++j) {
+            u32x4 o[RT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) o[r] = tile[((r * 4 + j) * 4 + lq) * 16 + (li ^ (lq * 4 + j))];
+            for (int r = 0; r < RT; ++r) o[r] = tile[((r * 4 + j) * 4 + lq) * 16 + (li ^ (lq * 4 + j))];
 #pragma unroll
-                for (int n = 0; n < kNt; ++n) {
-                    const u32x4 wv = weights_of(wt[n], j);
+            for (int n = 0; n < kNt; ++n) {
+                const u32x4 wv = weights_of(wt[n], j);
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) acc[n][r] = mfma(wv, o[r], acc[n][r]);
-                }
+                for (int r = 0; r < RT; ++r) acc[n][r] = mfma(wv, o[r], acc[n][r]);
             }
         }
-        ask_weights(wt, kt + 2 * kQuarters);
     };
-    for (uint32_t kt = quarter, base = 0; base < k_tiles; base += 2 * kQuarters, kt += 2 * kQuarters) {
-        step(ws[0], kt, 0);
-        if (base + kQuarters < k_tiles) step(ws[1], kt + kQuarters, 1);
+    // Whole k tiles, in rounds of four.  A quarter whose turn finds none left asks for the last one again and multiplies nothing: with loads inside
+    // of conditions the compiler's counts of what is in flight would make every round wait for all of it.
+    u32x4* tiles = lds + quarter * 2 * kTileVecs;
+    const uint32_t whole = K / kTile4K, rounds = ceil_div(whole, kQuarters);
+    if (rounds) {
+        RawWeights ws[2][kNt];
+        const auto nth = [&](uint32_t round) { return min(quarter + round * kQuarters, whole - 1); };
+        const auto step = [&](RawWeights (&wt)[kNt], uint32_t round) {
+            u32x4* tile = tiles + round % 2 * kTileVecs;
+            x.put(tile);
+            x.ask(nth(round + 1));
+            lds_barrier();
+            if (quarter + round * kQuarters < whole) multiply(wt, tile);
+            ask_weights(wt, nth(round + 2));
+        };
+        ask_weights(ws[0], nth(0));
+        x.ask(nth(0));
+        ask_weights(ws[1], nth(1));
+        for (uint32_t round = 0;;) {
+            step(ws[0], round);
+            if (++round == rounds) break;
+            step(ws[1], round);
+            if (++round == rounds) break;
+        }
+    }
+    if (whole < k_tiles) {
+        RawWeights wl[kNt];
+        ask_weights(wl, whole);
+        const bool mine = whole % kQuarters == quarter;
+        if (mine) x.ask_last(whole, K - whole * kTile4K);
+        lds_barrier();
+        if (mine) x.put(tiles);
+        lds_barrier();
+        if (mine) multiply(wl, tiles);
     }
     // a wave finishes RT of its slab's tiles, with the sums of the other quarters
     __syncthreads();
