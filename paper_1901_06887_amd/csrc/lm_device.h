@@ -58,6 +58,13 @@ template <typename T> __device__ __forceinline__ void store_some(T* p, uint32_t 
     for (uint32_t i = 0; i < 8; ++i) if (i < n) p[i] = (T)v[i];
 }
 
+// Between writes and reads of LDS by lanes of one wave.
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Over the wave, in every lane, by data-parallel-primitive moves (no LDS traffic): shifts by 1, 2, 4, 8 inside rows of 16 lanes, lane 15
 // of a row to the next, lane 31 to the upper half; the last lane has it all.
 template <typename F> __device__ __forceinline__ uint32_t wave_fold(uint32_t v, F f)

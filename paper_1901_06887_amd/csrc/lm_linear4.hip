@@ -157,12 +157,13 @@ template <Kind KIND, int RT, int NT> struct Step {
     }
 };
 
-// NaN stays NaN in both.
-__device__ __forceinline__ float activate4(float z, uint32_t act)
+// NaN stays NaN in both.  GELU: the library's erfc where fp32 is written; for bf16 the formula of the fully-connected layers (some 1e-7 off, a quarter of
+// the instructions), kept from multiplying an infinity by 0.
+__device__ __forceinline__ float activate4(float z, uint32_t act, uint32_t to_bf16)
 {
     if (act == MT_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (act == MT_ACT_GELU) return 0.5f * z * erfcf(-0.70710678f * z);
-    return z;
+    if (!to_bf16) return 0.5f * z * erfcf(-0.70710678f * z);
+    return fabsf(z) < 64.0f ? gelu(z) : z > 0.0f ? z : z < 0.0f ? -0.0f : z;
 }
 
 __device__ __forceinline__ void store4(__bf16* p, const f32x4& v) { *(Any<__bf16>::vec8*)p = Any<__bf16>::vec8{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
@@ -178,15 +179,37 @@ __device__ __forceinline__ void store_outputs(const Linear4Args& a, uint64_t row
         for (uint32_t i = 0; i < 4; ++i) if (n0 + i < N) y[i] = (Y)v[i];
 }
 
-// Four outputs of a row of the group: bias, activation, store.
+// The biases of four outputs; zeros where there are none.
+__device__ __forceinline__ f32x4 bias_of(const Linear4Args& a, const Group4& g, uint32_t n0)
+{
+    f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (!g.has_bias) return b;
+    const float* p = (const float*)(a.arena + g.off + matrix4_tiles_bytes(g.N, g.K));
+    if (n0 + 4 <= g.N) b = __builtin_bit_cast(f32x4, *(const Any<float>::vec16*)(p + n0));
+    else
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) if (n0 + i < g.N) b[i] = p[n0 + i];
+    return b;
+}
+
+// Four outputs of a row of the group: activation and store.
 __device__ __forceinline__ void finish_tile(const Linear4Args& a, const Group4& g, uint32_t n0, uint32_t in_group, f32x4 v)
 {
     if (in_group >= g.n_rows || n0 >= g.N) return;
-    const float* bias = g.has_bias ? (const float*)(a.arena + g.off + matrix4_tiles_bytes(g.N, g.K)) : nullptr;
+    if (a.act != MT_ACT_NONE) {
 #pragma unroll
-    for (uint32_t i = 0; i < 4; ++i) v[i] = activate4(v[i] + (bias && n0 + i < g.N ? bias[n0 + i] : 0.0f), a.act);
+        for (uint32_t i = 0; i < 4; ++i) v[i] = activate4(v[i], a.act, a.y_bf16);
+    }
     if (a.y_bf16) store_outputs<__bf16>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
     else store_outputs<float>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
+}
+
+// A workgroup's group: the last one that starts at or before it.
+__device__ __forceinline__ uint32_t group_of(const Linear4Args& a, uint32_t lane)
+{
+    if (a.n_groups == 1) return 0;
+    const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
+    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
 }
 
 constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles and add their sums up through LDS
@@ -196,13 +219,7 @@ template <Kind KIND, int RT, int NT, int DEPTH>
 __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // the group is the last one that starts at or before this workgroup
-    uint32_t gi = 0;
-    if (a.n_groups > 1) {
-        const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
-        gi = __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
-    }
-    const Group4& g = a.groups[gi];
+    const Group4& g = a.groups[group_of(a, lane)];
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_slabs = ceil_div(n_tiles, NT);
     const uint32_t local = blockIdx.x - g.wg_base;
@@ -266,6 +283,9 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
     }
 
     // tile t of the NT x RT is finished by wave t % 4
+    f32x4 bias[(NT * RT + kWaves4 - 1) / kWaves4];
+#pragma unroll
+    for (int i = 0; i < (NT * RT + kWaves4 - 1) / kWaves4; ++i) bias[i] = bias_of(a, g, (slab * NT + (i * kWaves4 + wave) / RT) * kTile4Rows + 4 * lq);
     __shared__ f32x4 part[kWaves4][NT * RT][64];
 #pragma unroll
     for (int t = 0; t < NT * RT; ++t) if (t % kWaves4 != (int)wave) part[wave][t][lane] = acc[t / RT][t % RT];
@@ -273,7 +293,7 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 #pragma unroll
     for (int t = 0; t < NT * RT; ++t) {
         if (t % kWaves4 != (int)wave) continue;
-        f32x4 v = acc[t / RT][t % RT];
+        f32x4 v = acc[t / RT][t % RT] + bias[t / kWaves4];
 #pragma unroll
         for (int o = 1; o < kWaves4; ++o) v += part[(wave + o) % kWaves4][t][lane];
         finish_tile(a, g, (slab * NT + t / RT) * kTile4Rows + 4 * lq, first_row + 16 * (t % RT) + li, v);
@@ -356,19 +376,16 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
     constexpr uint32_t kTileVecs = 16 * RT * 16;              // a k tile of the rows, in 16 bytes
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t quarter = wave / kSlabs, li = lane & 15, lq = lane >> 4;
-    uint32_t gi = 0;
-    if (a.n_groups > 1) {
-        const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
-        gi = __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
-    }
-    const Group4& g = a.groups[gi];
+    const Group4& g = a.groups[group_of(a, lane)];
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_wide = ceil_div(n_tiles, kNt * kSlabs), chunks = ceil_div(g.n_rows, 16 * RT);
     // workgroups eight apart share an XCD: they take the same outputs of one chunk of rows after the other
-    const uint32_t local = blockIdx.x - g.wg_base, in_eights = n_wide / 8 * 8 * chunks;
-    uint32_t wide, chunk;
-    if (local < in_eights) { wide = local / (8 * chunks) * 8 + local % 8; chunk = local / 8 % chunks; }
-    else { const uint32_t rest = local - in_eights, n = n_wide % 8; wide = n_wide - n + rest % n; chunk = rest / n; }
+    uint32_t wide = blockIdx.x - g.wg_base, chunk = 0;
+    if (chunks > 1) {
+        const uint32_t local = wide, in_eights = n_wide / 8 * 8 * chunks;
+        if (local < in_eights) { const uint32_t eighth = local / 8, n = eighth / chunks; wide = n * 8 + local % 8; chunk = eighth - n * chunks; }
+        else { const uint32_t rest = local - in_eights, n = n_wide % 8; chunk = rest / n; wide = n_wide - n + (rest - chunk * n); }
+    }
     const uint32_t slab = wide * kSlabs + wave % kSlabs, first_row = chunk * (16 * RT);
     const uint8_t* w[kNt];
 #pragma unroll
@@ -432,7 +449,10 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
         lds_barrier();
         if (mine) multiply(wl, tiles);
     }
-    // a wave finishes RT of its slab's tiles, with the sums of the other quarters
+    // quarter q finishes the tiles t with t % 4 = q of its slab, with the sums of the other quarters
+    f32x4 bias[kNt * RT / kQuarters];
+#pragma unroll
+    for (int i = 0; i < kNt * RT / kQuarters; ++i) bias[i] = bias_of(a, g, (slab * kNt + (i * kQuarters + quarter) / RT) * kTile4Rows + 4 * lq);
     __syncthreads();
     f32x4* part = (f32x4*)lds;
     const auto at = [&](uint32_t q, uint32_t t) { return ((q * kSlabs + wave % kSlabs) * (kNt * RT) + t) * 64 + lane; };
@@ -442,7 +462,7 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
 #pragma unroll
     for (int t = 0; t < kNt * RT; ++t) {
         if (t % kQuarters != (int)quarter) continue;
-        f32x4 v = acc[t / RT][t % RT];
+        f32x4 v = acc[t / RT][t % RT] + bias[t / kQuarters];
 #pragma unroll
         for (int o = 1; o < kQuarters; ++o) v += part[at((quarter + o) % kQuarters, t)];
         finish_tile(a, g, (slab * kNt + t / RT) * kTile4Rows + 4 * lq, first_row + 16 * (t % RT) + li, v);

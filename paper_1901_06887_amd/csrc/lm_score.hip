@@ -84,13 +84,6 @@ struct Sums {
     }
 };
 
-// Between writes and reads of LDS by lanes of one wave.
-__device__ __forceinline__ void wave_sync()
-{
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup", "local");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Entries among the kStep at `at` that are in front of `key`.
 constexpr uint32_t kStep = 8;
 __device__ __forceinline__ uint32_t in_front_of(uint64_t key, const uint64_t* at)
