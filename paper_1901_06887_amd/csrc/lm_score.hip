@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     const uint32_t* allowed = MASK ? a.allowed + row * a.allowed_stride : nullptr;
     const uint32_t part = WAVES == 1 ? 0 : blockIdx.y;
     const uint32_t part_end = min((uint64_t)(part + 1) * s.part_len, (uint64_t)a.classes);
-    const uint32_t wave_len = WAVES == 1 ? s.part_len : (s.part_len / WAVES + kChunk - 1) / kChunk * kChunk;
+    const uint32_t wave_len = WAVES == 1 ? s.part_len : ceil_div(s.part_len, WAVES * kChunk) * kChunk;
     uint32_t base = part * s.part_len + (WAVES == 1 ? 0 : wave * wave_len);
     const uint32_t mem_end = base < part_end ? min((uint64_t)base + wave_len, (uint64_t)part_end) : base;      // this wave's classes, and no more are read
     Raw<T> raw;
