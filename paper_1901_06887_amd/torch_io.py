@@ -76,8 +76,11 @@ def serve(ctx: B.Context, tenant_ids: torch.Tensor, inputs: torch.Tensor, out: O
 
 
 # ---- operators behind language models' answers ---------------------------------------------------
-_DTYPES = {torch.float32: B.MT_F32, torch.bfloat16: B.MT_BF16}
-_SCALES = (torch.float8_e8m0fnu, torch.uint8)
+# (A small call takes the GPU 3 to 5 us and the library's launch 3 us of the host, so the checks here look every attribute up once and the argument
+# blocks are packed in one go.)
+_F32, _BF16, _I32, _E4M3, _E8M0 = torch.float32, torch.bfloat16, torch.int32, torch.float8_e4m3fn, torch.float8_e8m0fnu
+_DTYPES = {_F32: B.MT_F32, _BF16: B.MT_BF16}
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -87,77 +90,87 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return code
 
 
-def _rows(t: torch.Tensor, what: str, rows: int, width: int, dtypes, device: int) -> int:
+def _rows(t: torch.Tensor, what: str, rows: int, width: int, dtype, device: int, or_dtype=None) -> int:
     """The elements between consecutive rows of a [rows][width] tensor on the device, whose rows are contiguous."""
-    if t.shape != (rows, width) or t.dtype not in dtypes or t.get_device() != device or (width > 1 and t.stride(1) != 1):
+    shape, strides, d = t.shape, t.stride(), t.dtype
+    if len(shape) != 2 or shape[0] != rows or shape[1] != width or (d is not dtype and d is not or_dtype) or t.get_device() != device or (strides[1] != 1 and width > 1):
         raise ValueError("%s: %s %s %s with strides %s; [%d, %d] of %s with contiguous rows on cuda:%d is wanted"
-                         % (what, tuple(t.shape), t.dtype, t.device, t.stride(), rows, width, " or ".join(str(d) for d in dtypes), device))
-    return t.stride(0) if rows > 1 else max(t.stride(0), width)
+                         % (what, tuple(shape), d, t.device, strides, rows, width, dtype, device))
+    return strides[0] if rows > 1 else width
 
 
-def _list(t: torch.Tensor, what: str, n: int, dtype, device: int) -> None:
-    if t.shape != (n,) or t.dtype != dtype or t.get_device() != device or (n > 1 and t.stride(0) != 1):
+def _list(t: torch.Tensor, what: str, n: int, dtype, device: int) -> int:
+    """The address of a contiguous list on the device."""
+    if t.shape != (n,) or t.dtype is not dtype or t.get_device() != device or (n > 1 and t.stride(0) != 1):
         raise ValueError("%s: %s %s %s; a contiguous [%d] of %s on cuda:%d is wanted" % (what, tuple(t.shape), t.dtype, t.device, n, dtype, device))
+    return t.data_ptr()
 
 
-def _stream(stream: Optional[torch.cuda.Stream], device: int) -> int:
-    # (the raw handle: a Stream object made per call takes as long as the rest of a small call)
-    return stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device)
+def _table(t: torch.Tensor, what: str, rows: int, width: int, dtype, device: int) -> int:
+    """The address of a contiguous [rows][width] tensor on the device."""
+    if _rows(t, what, rows, width, dtype, device) != width:
+        raise ValueError("%s is not contiguous" % what)
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, what: str):
+    if t.dim() != 2:
+        raise ValueError("%s: %s; two dimensions are wanted" % (what, tuple(t.shape)))
+    return t.shape
 
 
 def add_norm(ctx: B.Context, x: torch.Tensor, residual: Optional[torch.Tensor] = None, gain: Optional[torch.Tensor] = None,
              gain_ids: Optional[torch.Tensor] = None, eps: float = 1e-6, sum_out: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
              out8: Optional[torch.Tensor] = None, out8_scales: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """mt_add_norm on the given (or current) stream: h = x + residual into sum_out, h / rms(h) * gain into out (in x's type) and, as
-    8-bit rows, into out8 (float8_e4m3fn) and out8_scales (float8_e8m0fnu).  gain: float32 [width], or [tenants, width] with
+    8-bit rows, into out8 (float8_e4m3fn) and out8_scales (float8_e8m0fnu, or its bytes).  gain: float32 [width], or [tenants, width] with
     gain_ids int32 [rows]."""
-    code, (rows, width), dev = _dtype(x, "rows"), x.shape, x.get_device()
-    same = (x.dtype,)
-    a = B.mt_norm_args()
-    a.rows, a.width, a.dtype, a.eps = rows, width, code, eps
-    a.x, a.x_stride = x.data_ptr(), _rows(x, "x", rows, width, same, ctx.cfg.device)
+    (rows, width), dev, dtype = _matrix(x, "x"), ctx.device, x.dtype
+    code = _dtype(x, "rows")
+    x_stride = _rows(x, "x", rows, width, dtype, dev)
+    residual_p = residual_stride = gain_p = gain_stride = n_gains = ids_p = sum_p = sum_stride = y_p = y_stride = y8_p = y8_stride = scales_p = scales_stride = 0
     if residual is not None:
-        a.residual, a.residual_stride = residual.data_ptr(), _rows(residual, "residual", rows, width, same, dev)
+        residual_p, residual_stride = residual.data_ptr(), _rows(residual, "residual", rows, width, dtype, dev)
     if gain is not None:
-        g = gain if gain.dim() == 2 else gain.unsqueeze(0)
-        a.gain, a.gain_stride, a.n_gains = g.data_ptr(), _rows(g, "gain", g.shape[0], width, (torch.float32,), dev), g.shape[0]
+        if gain.dim() == 1:
+            gain = gain.unsqueeze(0)
+        n_gains = gain.shape[0]
+        gain_p, gain_stride = gain.data_ptr(), _rows(gain, "gain", n_gains, width, _F32, dev)
     if gain_ids is not None:
-        _list(gain_ids, "gain_ids", rows, torch.int32, dev)
-        a.gain_ids = gain_ids.data_ptr()
+        ids_p = _list(gain_ids, "gain_ids", rows, _I32, dev)
     if sum_out is not None:
-        a.sum, a.sum_stride = sum_out.data_ptr(), _rows(sum_out, "sum_out", rows, width, same, dev)
+        sum_p, sum_stride = sum_out.data_ptr(), _rows(sum_out, "sum_out", rows, width, dtype, dev)
     if out is not None:
-        a.y, a.y_stride = out.data_ptr(), _rows(out, "out", rows, width, same, dev)
+        y_p, y_stride = out.data_ptr(), _rows(out, "out", rows, width, dtype, dev)
     if out8 is not None:
-        a.y8, a.y8_stride = out8.data_ptr(), _rows(out8, "out8", rows, width, (torch.float8_e4m3fn,), dev)
+        y8_p, y8_stride = out8.data_ptr(), _rows(out8, "out8", rows, width, _E4M3, dev)
     if out8_scales is not None:
-        a.y8_scales, a.y8_scales_stride = out8_scales.data_ptr(), _rows(out8_scales, "out8_scales", rows, -(-width // B.MT_MX_BLOCK), _SCALES, dev)
-    ctx.add_norm(_stream(stream, dev), a)
+        scales_p, scales_stride = out8_scales.data_ptr(), _rows(out8_scales, "out8_scales", rows, (width + 31) // 32, _E8M0, dev, torch.uint8)
+    ctx.add_norm(stream.cuda_stream if stream is not None else _raw_stream(dev),
+                 B.pack_norm_args(x.data_ptr(), residual_p, gain_p, ids_p, sum_p, y_p, y8_p, scales_p, x_stride, residual_stride, gain_stride, sum_stride, y_stride,
+                                  y8_stride, scales_stride, rows, width, n_gains, code, eps, 0))
 
 
 def linear4(ctx: B.Context, groups, x: torch.Tensor, out: torch.Tensor, x_scales: Optional[torch.Tensor] = None, act: int = B.MT_ACT_NONE,
             stream: Optional[torch.cuda.Stream] = None) -> None:
     """mt_linear4 on the given (or current) stream: the rows of every group (row_groups) times its matrix, into out (float32 or bfloat16).
     x: float32, bfloat16, or float8_e4m3fn with x_scales."""
-    rows, width = x.shape
-    dev = ctx.cfg.device
-    a = B.mt_linear4_args()
-    if x.dtype == torch.float8_e4m3fn:
-        a.x_dtype = B.MT_MX8
+    (rows, width), dev, dtype = _matrix(x, "x"), ctx.device, x.dtype
+    scales_p = scales_stride = 0
+    if dtype is _E4M3:
+        code = B.MT_MX8
         if x_scales is None:
             raise ValueError("8-bit rows come with their scales")
-        a.x_scales, a.x_scales_stride = x_scales.data_ptr(), _rows(x_scales, "x_scales", rows, -(-width // B.MT_MX_BLOCK), _SCALES, dev)
+        scales_p, scales_stride = x_scales.data_ptr(), _rows(x_scales, "x_scales", rows, (width + 31) // 32, _E8M0, dev, torch.uint8)
     else:
-        a.x_dtype = _dtype(x, "rows")
+        code = _dtype(x, "rows")
         if x_scales is not None:
             raise ValueError("scales come with 8-bit rows only")
-    a.rows, a.act, a.y_dtype = rows, act, _dtype(out, "out")
-    a.x, a.y = x.data_ptr(), out.data_ptr()
-    # (a matrix may be narrower than the rows, so the widths that the strides are checked against are these)
-    a.x_stride, a.y_stride = _rows(x, "x", rows, width, (x.dtype,), dev), _rows(out, "out", rows, out.shape[1], (out.dtype,), dev)
-    if rows <= 1:
-        a.x_stride, a.y_stride = width, out.shape[1]
-    ctx.linear4(_stream(stream, dev), a, groups)
+    n = _matrix(out, "out")[1]
+    # (a matrix may be narrower than the rows: its sizes are checked against the strides, which for one row are the widths)
+    ctx.linear4(stream.cuda_stream if stream is not None else _raw_stream(dev),
+                B.pack_linear4_args(x.data_ptr(), scales_p, out.data_ptr(), _rows(x, "x", rows, width, dtype, dev), scales_stride,
+                                    _rows(out, "out", rows, n, out.dtype, dev), rows, code, _dtype(out, "out"), act), groups)
 
 
 @dataclass
@@ -182,33 +195,30 @@ def score(ctx: B.Context, logits: torch.Tensor, out: Scores, given: Optional[tor
           allowed: Optional[torch.Tensor] = None, temperature: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> Scores:
     """mt_score on the given (or current) stream: what rows of logits say about given classes (int32 [rows, n_given]), their entropy and
     the best alternatives.  n_classes: int32 [rows]; allowed: int32 [rows, words], a bit for every class."""
-    code, (rows, classes), dev = _dtype(logits, "logits"), logits.shape, ctx.cfg.device
-    a = B.mt_score_args()
-    a.rows, a.classes, a.dtype, a.temperature = rows, classes, code, temperature
-    a.logits, a.row_stride = logits.data_ptr(), _rows(logits, "logits", rows, classes, (logits.dtype,), dev)
-    _list(out.entropy, "entropy", rows, torch.float32, dev)
-    a.entropy = out.entropy.data_ptr()
+    (rows, classes), dev = _matrix(logits, "logits"), ctx.device
+    code = _dtype(logits, "logits")
+    stride = _rows(logits, "logits", rows, classes, logits.dtype, dev)
+    n_p = allowed_p = allowed_stride = given_p = n_given = lp_p = ranks_p = top = ids_p = top_p = 0
+    entropy_p = _list(out.entropy, "entropy", rows, _F32, dev)
     if n_classes is not None:
-        _list(n_classes, "n_classes", rows, torch.int32, dev)
-        a.n_classes = n_classes.data_ptr()
+        n_p = _list(n_classes, "n_classes", rows, _I32, dev)
     if allowed is not None:
-        if allowed.dim() != 2 or allowed.shape[1] < -(-classes // 32):
+        words = _matrix(allowed, "allowed")[1]
+        if words < (classes + 31) // 32:
             raise ValueError("allowed: %s for %d rows of %d classes" % (tuple(allowed.shape), rows, classes))
-        a.allowed, a.allowed_stride = allowed.data_ptr(), _rows(allowed, "allowed", rows, allowed.shape[1], (torch.int32,), dev)
-    if (given is None) != (out.given_ranks is None):
+        allowed_p, allowed_stride = allowed.data_ptr(), _rows(allowed, "allowed", rows, words, _I32, dev)
+    ranks = out.given_ranks
+    if (given is None) != (ranks is None):
         raise ValueError("given classes and their outputs come together")
     if given is not None:
-        n = out.given_ranks.shape[1]
-        for t, what, d in ((given, "given", torch.int32), (out.given_ranks, "given_ranks", torch.int32), (out.given_logprobs, "given_logprobs", torch.float32)):
-            if _rows(t, what, rows, n, (d,), dev) != n:
-                raise ValueError("%s is not contiguous" % what)
-        a.n_given, a.given, a.given_ranks, a.given_logprobs = n, given.data_ptr(), out.given_ranks.data_ptr(), out.given_logprobs.data_ptr()
+        n_given = ranks.shape[1]
+        given_p, ranks_p = _table(given, "given", rows, n_given, _I32, dev), _table(ranks, "given_ranks", rows, n_given, _I32, dev)
+        lp_p = _table(out.given_logprobs, "given_logprobs", rows, n_given, _F32, dev)
     if out.top_ids is not None:
-        n = out.top_ids.shape[1]
-        for t, what, d in ((out.top_ids, "top_ids", torch.int32), (out.top_logprobs, "top_logprobs", torch.float32)):
-            if _rows(t, what, rows, n, (d,), dev) != n:
-                raise ValueError("%s is not contiguous" % what)
-        a.top, a.top_ids, a.top_logprobs = n, out.top_ids.data_ptr(), out.top_logprobs.data_ptr()
-    a.scratch, a.scratch_bytes = out.scratch.data_ptr(), out.scratch.numel()
-    ctx.score(_stream(stream, dev), a)
+        top = out.top_ids.shape[1]
+        ids_p, top_p = _table(out.top_ids, "top_ids", rows, top, _I32, dev), _table(out.top_logprobs, "top_logprobs", rows, top, _F32, dev)
+    scratch = out.scratch
+    ctx.score(stream.cuda_stream if stream is not None else _raw_stream(dev),
+              B.pack_score_args(logits.data_ptr(), n_p, allowed_p, given_p, lp_p, ranks_p, entropy_p, ids_p, top_p, scratch.data_ptr(), scratch.numel(), stride,
+                                allowed_stride, rows, classes, n_given, top, code, temperature))
     return out

@@ -172,3 +172,10 @@ def test_score_refuses():
     lib = B.load_library()
     assert lib.mt_score(c._h, None, None) == 1 and lib.mt_score(None, None, ctypes.byref(score_args())) == 1
     c.close()
+
+
+def test_packed_blocks_are_the_structures():
+    """The bytes that the packing functions make are those of the structure filled field by field."""
+    for pack, cls in ((B.pack_norm_args, B.mt_norm_args), (B.pack_linear4_args, B.mt_linear4_args), (B.pack_score_args, B.mt_score_args)):
+        values = [0.5 if t is ctypes.c_float else i + 3 for i, (_, t) in enumerate(cls._fields_)]
+        assert pack(*values) == bytes(cls(*values))
