@@ -144,8 +144,8 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
     if (a->act > MT_ACT_GELU) return ctx_fail(c, MT_EUNSUPPORTED, "activation %u", a->act);
     if (a->rows && (!a->x || !a->y)) return ctx_fail(c, MT_EINVAL, "null rows");
     if (a->rows && (a->x_dtype == MT_MX8) != (a->x_scales != nullptr)) return ctx_fail(c, MT_EINVAL, "scales come with 8-bit rows, and only with them");
-    uint64_t next = 0, tiles = 0;
-    uint32_t most_rows = 0, least_kt = UINT32_MAX;
+    uint64_t next = 0, row_tiles = 0;      // tiles of 16 outputs x 16 rows
+    uint32_t most_rows = 0, most_k = 0;
     for (uint32_t g = 0; g < n_groups; ++g) {
         const mt_row_group& r = groups[g];
         if (r.matrix >= v.matrices->size() || !(*v.matrices)[r.matrix].used) return ctx_fail(c, MT_ENOTFOUND, "group %u: no matrix %u", g, r.matrix);
@@ -157,14 +157,14 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
         next = (uint64_t)r.first_row + r.n_rows;
         if (r.n_rows == 0) continue;
         most_rows = std::max(most_rows, r.n_rows);
-        tiles += div_up(m.N, kTile4Rows);
-        least_kt = std::min(least_kt, div_up(m.K, kTile4K));
+        most_k = std::max(most_k, m.K);
+        row_tiles += (uint64_t)div_up(m.N, kTile4Rows) * div_up(r.n_rows, kTile4Rows);
     }
     if (v.host_only) return ctx_fail(c, MT_ESTATE, "host-only context cannot run");
     if (most_rows == 0) return MT_OK;
     LM_TRY(c, hipSetDevice(v.device));
 
-    const Linear4Shape shape = linear4_shape(tiles, least_kt, most_rows, v.n_cus, a->x_dtype);
+    const Linear4Shape shape = linear4_shape(row_tiles, most_rows, most_k, v.n_cus, a->x_dtype);
     Linear4Args k;
     k.arena = v.arena; k.x = a->x; k.x_scales = a->x_scales; k.y = a->y;
     k.x_stride = a->x_stride; k.x_scales_stride = a->x_scales_stride; k.y_stride = a->y_stride;

@@ -29,6 +29,19 @@ __device__ __forceinline__ void split3(float x, uint32_t (&part)[3])
     if (special) { part[0] |= (b & 0xffffu) ? 0x400000u : 0u; part[1] = part[2] = 0; }
 }
 
+// Four of them, packed.
+__device__ __forceinline__ void split3(const u32x4& x, uint32_t (&part)[3][2])
+{
+    const f32x4 f = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t lo[3], hi[3];
+        split3(f[2 * i], lo); split3(f[2 * i + 1], hi);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) part[q][i] = lo[q] >> 16 | hi[q];
+    }
+}
+
 // 2^(byte - 127); the smallest is subnormal, the largest byte is NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte == 0xff ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u); }
 // Eight 8-bit values, scaled, as bf16.
@@ -38,49 +51,63 @@ __device__ __forceinline__ u32x4 eight_of(uint32_t lo, uint32_t hi, float s)
                  __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false)), __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true))};
 }
 
+// 16 bytes of a row, from any element's address.
+template <Kind KIND> __device__ __forceinline__ u32x4 load16(const uint8_t* p)
+{
+    if constexpr (KIND == kRowsF32) return *(const Any<float>::vec16*)p;
+    else if constexpr (KIND == kRowsBf16) return *(const Any<__bf16>::vec16*)p;
+    else return *(const Any<uint8_t>::vec16*)p;
+}
+
+// The same from value `first` of a last k tile that is not whole: `left` values from `tile` on, zeros behind them.  A row of at least 16 bytes is read up to
+// its end and shifted down: one load for every lane, where loads of single values would each wait for the one before.
+template <Kind KIND> __device__ __forceinline__ u32x4 load16_last(const uint8_t* tile, uint32_t first, uint32_t left, uint32_t K)
+{
+    constexpr uint32_t es = row_size(KIND), kEach = 16 / es;
+    u32x4 v;
+    if (K >= kEach) {
+        const int32_t over = max((int32_t)(first + kEach) - (int32_t)left, 0);      // values past the end (signed: from an unsigned difference the compiler took it that there are some)
+        v = load16<KIND>(tile + (int64_t)((int32_t)first - over) * es);
+        const uint32_t bytes = (uint32_t)min(over, (int32_t)kEach) * es;
+        if (bytes & 8) v = u32x4{v[2], v[3], 0, 0};
+        if (bytes & 4) v = u32x4{v[1], v[2], v[3], 0};
+        if constexpr (es < 4)
+            v = u32x4{__builtin_amdgcn_alignbyte(v[1], v[0], bytes & 3), __builtin_amdgcn_alignbyte(v[2], v[1], bytes & 3), __builtin_amdgcn_alignbyte(v[3], v[2], bytes & 3),
+                      __builtin_amdgcn_alignbyte(0, v[3], bytes & 3)};
+        if (bytes == 16) v = u32x4{0, 0, 0, 0};
+    } else {
+        v = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; ++e) {
+            const uint32_t at = min(first + e, left - 1);
+            uint32_t one;
+            if constexpr (es == 4) one = ((const uint32_t*)tile)[at];
+            else if constexpr (es == 2) one = ((const uint16_t*)tile)[at];
+            else one = tile[at];
+            if (first + e < left) v[e * es / 4] |= one << (8 * (e * es % 4));
+        }
+    }
+    return v;
+}
+
 // A lane's 32 values of a row as they come from memory.
 template <Kind KIND> struct RawRow {
     static constexpr uint32_t kVecs = row_size(KIND) * 2;      // of 16 bytes
     u32x4 v[kVecs];
     uint32_t scale;
 
-    // p: the lane's k block
-    __device__ __forceinline__ void load(const uint8_t* p, const uint8_t* scale_at)
+    // tile: the row's values of the k tile; its scales likewise
+    __device__ __forceinline__ void load(const uint8_t* tile, const uint8_t* scales, uint32_t lq)
     {
 #pragma unroll
-        for (uint32_t i = 0; i < kVecs; ++i) {
-            const uint8_t* q = p + 16 * i;
-            if constexpr (KIND == kRowsF32) v[i] = *(const Any<float>::vec16*)q;
-            else if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
-            else v[i] = *(const Any<uint8_t>::vec16*)q;
-        }
-        if constexpr (KIND == kRowsMx8) scale = *scale_at;
+        for (uint32_t i = 0; i < kVecs; ++i) v[i] = load16<KIND>(tile + lq * (32 * row_size(KIND)) + 16 * i);
+        if constexpr (KIND == kRowsMx8) scale = scales[lq];
     }
-
-    // The last k tile, of `left` values from k block 0 on: zeros behind them.
-    __device__ __forceinline__ void load_last(const uint8_t* p, const uint8_t* scale_at, uint32_t lq, uint32_t left)
+    __device__ __forceinline__ void load_last(const uint8_t* tile, const uint8_t* scales, uint32_t lq, uint32_t left, uint32_t K)
     {
-        constexpr uint32_t es = row_size(KIND), kEach = 16 / es;                // values of a vector
 #pragma unroll
-        for (uint32_t i = 0; i < kVecs; ++i) {
-            const uint32_t first = lq * 32 + kEach * i;     // ... its first one
-            const uint8_t* q = p + 16 * i;
-            v[i] = u32x4{0, 0, 0, 0};
-            if (first + kEach <= left) {
-                if constexpr (KIND == kRowsF32) v[i] = *(const Any<float>::vec16*)q;
-                else if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
-                else v[i] = *(const Any<uint8_t>::vec16*)q;
-            } else if (first < left) {
-#pragma unroll
-                for (uint32_t e = 0; e < kEach; ++e)
-                    if (first + e < left) {
-                        if constexpr (es == 4) v[i][e] = ((const uint32_t*)q)[e];
-                        else if constexpr (es == 2) v[i][e / 2] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e % 2));
-                        else v[i][e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
-                    }
-            }
-        }
-        if constexpr (KIND == kRowsMx8) scale = lq * 32 < left ? *scale_at : 127;
+        for (uint32_t i = 0; i < kVecs; ++i) v[i] = load16_last<KIND>(tile, lq * 32 + 16 / row_size(KIND) * i, left, K);
+        if constexpr (KIND == kRowsMx8) scale = scales[min(lq, (left - 1) / MT_MX_BLOCK)];
     }
 };
 
@@ -96,14 +123,10 @@ template <Kind KIND> struct RowOperand {
             else if constexpr (KIND == kRowsF32) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const f32x4 f = __builtin_bit_cast(f32x4, r.v[2 * j + h]);
+                    uint32_t part[3][2];
+                    split3(r.v[2 * j + h], part);
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t lo[3], hi[3];
-                        split3(f[2 * i], lo); split3(f[2 * i + 1], hi);
-#pragma unroll
-                        for (int q = 0; q < 3; ++q) v[q][j][2 * h + i] = lo[q] >> 16 | hi[q];
-                    }
+                    for (int q = 0; q < 3; ++q) { v[q][j][2 * h] = part[q][0]; v[q][j][2 * h + 1] = part[q][1]; }
                 }
             } else if constexpr (KIND == kRowsMx8) {
                 v[0][j] = eight_of(r.v[j / 2][2 * (j % 2)], r.v[j / 2][2 * (j % 2) + 1], scale_of(r.scale));
@@ -132,28 +155,25 @@ __device__ __forceinline__ f32x4 mfma(const u32x4& w, const u32x4& x, const f32x
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
 }
 
-// One k tile: NT tiles of 16 outputs, RT tiles of 16 rows.
-template <Kind KIND, int RT, int NT> struct Step {
+// One k tile: NT tiles of 16 outputs times 16 rows.
+template <Kind KIND, int NT> struct Step {
     RawWeights w[NT];
-    RawRow<KIND> x[RT];
+    RawRow<KIND> x;
 
-    __device__ __forceinline__ void multiply(f32x4 (&acc)[NT][RT]) const
+    __device__ __forceinline__ void multiply(f32x4 (&acc)[NT]) const
     {
+        const RowOperand<KIND> o(x);
         u32x4 wv[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) wv[n][j] = weights_of(w[n], j);
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const RowOperand<KIND> o(x[r]);
+        for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
 #pragma unroll
-            for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) acc[n][r] = mfma(wv[n][j], o.v[p][j], acc[n][r]);
-        }
+                for (int n = 0; n < NT; ++n) acc[n] = mfma(wv[n][j], o.v[p][j], acc[n]);
     }
 };
 
@@ -214,8 +234,8 @@ __device__ __forceinline__ uint32_t group_of(const Linear4Args& a, uint32_t lane
 
 constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles and add their sums up through LDS
 
-// A workgroup serves 16 NT outputs of 16 RT rows of a group; a wave asks for DEPTH k tiles at a time, the next ones before it multiplies.
-template <Kind KIND, int RT, int NT, int DEPTH>
+// A workgroup serves 16 NT outputs of 16 rows of a group; a wave asks for DEPTH k tiles at a time, the next ones before it multiplies.
+template <Kind KIND, int NT, int DEPTH>
 __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -223,38 +243,31 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_slabs = ceil_div(n_tiles, NT);
     const uint32_t local = blockIdx.x - g.wg_base;
-    const uint32_t slab = local % n_slabs, first_row = local / n_slabs * (16 * RT);
+    const uint32_t slab = local % n_slabs, first_row = local / n_slabs * kTile4Rows;
     const uint32_t li = lane & 15, lq = lane >> 4;
     const uint8_t* w[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) w[n] = a.arena + g.off + (uint64_t)min(slab * NT + n, n_tiles - 1) * k_tiles * kTile4Bytes;
-    const uint8_t *x[RT], *xs[RT];
+    const uint64_t row = (uint64_t)g.row0 + min(first_row + li, g.n_rows - 1);
+    const uint8_t* x = (const uint8_t*)a.x + row * a.x_stride * row_size(KIND);
+    const uint8_t* xs = a.x_scales + row * a.x_scales_stride;
+    f32x4 acc[NT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const uint64_t row = (uint64_t)g.row0 + min(first_row + 16 * r + li, g.n_rows - 1);
-        x[r] = (const uint8_t*)a.x + row * a.x_stride * row_size(KIND) + lq * (32 * row_size(KIND));
-        xs[r] = a.x_scales + row * a.x_scales_stride + lq;
-    }
-    f32x4 acc[NT][RT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int r = 0; r < RT; ++r) acc[n][r] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
     // whole k tiles: this wave's are wave, wave + 4, ...
     const uint32_t whole = K / kTile4K;
-    Step<KIND, RT, NT> at[2][DEPTH];
-    const auto ask = [&](Step<KIND, RT, NT> (&to)[DEPTH], uint32_t kt) {
+    Step<KIND, NT> at[2][DEPTH];
+    const auto ask = [&](Step<KIND, NT> (&to)[DEPTH], uint32_t kt) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             const uint32_t t = min(kt + d * kWaves4, whole - 1);
 #pragma unroll
             for (int n = 0; n < NT; ++n) to[d].w[n] = load_weights(w[n] + (uint64_t)t * kTile4Bytes, lane);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) to[d].x[r].load(x[r] + t * (kTile4K * row_size(KIND)), xs[r] + t * 4);
+            to[d].x.load(x + t * (kTile4K * row_size(KIND)), xs + t * 4, lq);
         }
     };
-    const auto use = [&](const Step<KIND, RT, NT> (&of)[DEPTH], uint32_t kt) {
+    const auto use = [&](const Step<KIND, NT> (&of)[DEPTH], uint32_t kt) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) if (d == 0 || kt + d * kWaves4 < whole) of[d].multiply(acc);
     };
@@ -274,29 +287,28 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
         }
     }
     if (whole < k_tiles && whole % kWaves4 == wave) {           // the last one, where it is not whole
-        Step<KIND, RT, NT> last;
+        Step<KIND, NT> last;
 #pragma unroll
         for (int n = 0; n < NT; ++n) last.w[n] = load_weights(w[n] + (uint64_t)whole * kTile4Bytes, lane);
-#pragma unroll
-        for (int r = 0; r < RT; ++r) last.x[r].load_last(x[r] + (uint64_t)whole * (kTile4K * row_size(KIND)), xs[r] + whole * 4, lq, K - whole * kTile4K);
+        last.x.load_last(x + (uint64_t)whole * (kTile4K * row_size(KIND)), xs + whole * 4, lq, K - whole * kTile4K, K);
         last.multiply(acc);
     }
 
-    // tile t of the NT x RT is finished by wave t % 4
-    f32x4 bias[(NT * RT + kWaves4 - 1) / kWaves4];
+    // tile n is finished by wave n
+    static_assert(NT <= kWaves4, "a wave finishes one tile at most");
+    const f32x4 bias = bias_of(a, g, (slab * NT + wave) * kTile4Rows + 4 * lq);
+    __shared__ f32x4 part[kWaves4][NT][64];
 #pragma unroll
-    for (int i = 0; i < (NT * RT + kWaves4 - 1) / kWaves4; ++i) bias[i] = bias_of(a, g, (slab * NT + (i * kWaves4 + wave) / RT) * kTile4Rows + 4 * lq);
-    __shared__ f32x4 part[kWaves4][NT * RT][64];
-#pragma unroll
-    for (int t = 0; t < NT * RT; ++t) if (t % kWaves4 != (int)wave) part[wave][t][lane] = acc[t / RT][t % RT];
+    for (int n = 0; n < NT; ++n) if (n != (int)wave) part[wave][n][lane] = acc[n];
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < NT * RT; ++t) {
-        if (t % kWaves4 != (int)wave) continue;
-        f32x4 v = acc[t / RT][t % RT] + bias[t / kWaves4];
+    for (int n = 0; n < NT; ++n) {
+        if (n != (int)wave) continue;
+        f32x4 v = acc[n] + bias;
 #pragma unroll
-        for (int o = 1; o < kWaves4; ++o) v += part[(wave + o) % kWaves4][t][lane];
-        finish_tile(a, g, (slab * NT + t / RT) * kTile4Rows + 4 * lq, first_row + 16 * (t % RT) + li, v);
+        for (int o = 1; o < kWaves4; ++o) v += part[(wave + o) % kWaves4][n][lane];
+        // lane l: row l % 16, outputs 4 (l / 16) .. + 3 of the tile
+        finish_tile(a, g, (slab * NT + n) * kTile4Rows + 4 * lq, first_row + li, v);
     }
 }
 
@@ -321,33 +333,24 @@ template <Kind KIND, int RT> struct RowFetch {
 #pragma unroll
         for (uint32_t i = 0; i < kPasses; ++i) {
             const uint64_t row = (uint64_t)g.row0 + min(first_row + row0 + i * kRowsAtOnce, g.n_rows - 1);
-            p[i] = (const uint8_t*)a.x + row * a.x_stride * row_size(KIND) + u * 16;
-            if constexpr (KIND == kRowsMx8) ps[i] = a.x_scales + row * a.x_scales_stride + u / 2;
+            p[i] = (const uint8_t*)a.x + row * a.x_stride * row_size(KIND);
+            if constexpr (KIND == kRowsMx8) ps[i] = a.x_scales + row * a.x_scales_stride;
         }
     }
     __device__ __forceinline__ void ask(uint32_t kt)
     {
 #pragma unroll
         for (uint32_t i = 0; i < kPasses; ++i) {
-            const uint8_t* q = p[i] + kt * (kTile4K * row_size(KIND));
-            if constexpr (KIND == kRowsBf16) v[i] = *(const Any<__bf16>::vec16*)q;
-            else { v[i] = *(const Any<uint8_t>::vec16*)q; scale[i] = ps[i][kt * (kTile4K / MT_MX_BLOCK)]; }
+            v[i] = load16<KIND>(p[i] + kt * (kTile4K * row_size(KIND)) + u * 16);
+            if constexpr (KIND == kRowsMx8) scale[i] = ps[i][kt * (kTile4K / MT_MX_BLOCK) + u / 2];
         }
     }
-    // The last k tile where it is not whole, `left` values long: zeros behind them.
-    __device__ __forceinline__ void ask_last(uint32_t kt, uint32_t left)
+    __device__ __forceinline__ void ask_last(uint32_t kt, uint32_t left, uint32_t K)
     {
 #pragma unroll
         for (uint32_t i = 0; i < kPasses; ++i) {
-            const uint8_t* q = p[i] + kt * (kTile4K * row_size(KIND));
-            v[i] = u32x4{0, 0, 0, 0};
-#pragma unroll
-            for (uint32_t e = 0; e < kPer; ++e)
-                if (u * kPer + e < left) {
-                    if constexpr (KIND == kRowsBf16) v[i][e / 2] |= (uint32_t)((const uint16_t*)q)[e] << (16 * (e % 2));
-                    else v[i][e / 4] |= (uint32_t)q[e] << (8 * (e % 4));
-                }
-            if constexpr (KIND == kRowsMx8) scale[i] = u * kPer < left ? ps[i][kt * (kTile4K / MT_MX_BLOCK)] : 127;
+            v[i] = load16_last<KIND>(p[i] + kt * (kTile4K * row_size(KIND)), u * kPer, left, K);
+            if constexpr (KIND == kRowsMx8) scale[i] = ps[i][kt * (kTile4K / MT_MX_BLOCK) + min(u / 2, (left - 1) / MT_MX_BLOCK)];
         }
     }
     static __device__ __forceinline__ uint32_t place(uint32_t row, uint32_t c)      // in 16 bytes
@@ -360,7 +363,12 @@ template <Kind KIND, int RT> struct RowFetch {
         for (uint32_t i = 0; i < kPasses; ++i) {
             const uint32_t row = row0 + i * kRowsAtOnce;
             if constexpr (KIND == kRowsBf16) to[place(row, u)] = v[i];
-            else {
+            else if constexpr (KIND == kRowsF32) {
+                uint32_t part[3][2];
+                split3(v[i], part);
+#pragma unroll
+                for (uint32_t q = 0; q < 3; ++q) *((u32x2*)(to + q * (16 * RT * 16) + place(row, u / 2)) + u % 2) = u32x2{part[q][0], part[q][1]};
+            } else {
                 const float s = scale_of(scale[i]);
                 to[place(row, 2 * u)] = eight_of(v[i][0], v[i][1], s);
                 to[place(row, 2 * u + 1)] = eight_of(v[i][2], v[i][3], s);
@@ -373,7 +381,7 @@ template <Kind KIND, int RT>
 __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
 {
     extern __shared__ __attribute__((aligned(16))) u32x4 lds[];
-    constexpr uint32_t kTileVecs = 16 * RT * 16;              // a k tile of the rows, in 16 bytes
+    constexpr uint32_t kParts = KIND == kRowsF32 ? 3 : 1, kPartVecs = 16 * RT * 16, kTileVecs = kParts * kPartVecs;      // a k tile of the rows, in 16 bytes
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t quarter = wave / kSlabs, li = lane & 15, lq = lane >> 4;
     const Group4& g = a.groups[group_of(a, lane)];
@@ -403,14 +411,18 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
     const auto multiply = [&](const RawWeights (&wt)[kNt], const u32x4* tile) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            u32x4 o[RT];
+            u32x4 wv[kNt];
 #pragma unroll
-            for (int r = 0; r < RT; ++r) o[r] = tile[((r * 4 + j) * 4 + lq) * 16 + (li ^ (lq * 4 + j))];
+            for (int n = 0; n < kNt; ++n) wv[n] = weights_of(wt[n], j);
 #pragma unroll
-            for (int n = 0; n < kNt; ++n) {
-                const u32x4 wv = weights_of(wt[n], j);
+            for (int p = kParts - 1; p >= 0; --p) {
+                u32x4 o[RT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) acc[n][r] = mfma(wv, o[r], acc[n][r]);
+                for (int r = 0; r < RT; ++r) o[r] = tile[p * kPartVecs + ((r * 4 + j) * 4 + lq) * 16 + (li ^ (lq * 4 + j))];
+#pragma unroll
+                for (int n = 0; n < kNt; ++n)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[n][r] = mfma(wv[n], o[r], acc[n][r]);
             }
         }
     };
@@ -443,7 +455,7 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
         RawWeights wl[kNt];
         ask_weights(wl, whole);
         const bool mine = whole % kQuarters == quarter;
-        if (mine) x.ask_last(whole, K - whole * kTile4K);
+        if (mine) x.ask_last(whole, K - whole * kTile4K, K);
         lds_barrier();
         if (mine) x.put(tiles);
         lds_barrier();
@@ -468,47 +480,66 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
         finish_tile(a, g, (slab * kNt + t / RT) * kTile4Rows + 4 * lq, first_row + 16 * (t % RT) + li, v);
     }
 }
-template <int RT> constexpr uint32_t rows_lds() { return kQuarters * kSlabs * (kNt * RT) * 1024; }      // the sums at the end; both buffers of rows take no more
-static_assert(rows_lds<4>() >= kQuarters * 2 * 64 * 256 && rows_lds<4>() <= 160 * 1024, "LDS");
+// both buffers of rows, or the sums at the end
+template <Kind KIND, int RT> constexpr uint32_t rows_lds()
+{
+    constexpr uint32_t rows = kQuarters * 2 * 16 * RT * 256 * (KIND == kRowsF32 ? 3 : 1), sums = kQuarters * kSlabs * (kNt * RT) * 1024;
+    static_assert(rows <= 160 * 1024 && sums <= 160 * 1024, "LDS");
+    return rows > sums ? rows : sums;
+}
 
-template <Kind KIND, int RT, int NT, int DEPTH>
+template <Kind KIND, int NT, int DEPTH>
 hipError_t go(const Linear4Args& a, uint32_t grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((linear4_kernel<KIND, RT, NT, DEPTH>), dim3(grid), dim3(kWaves4 * 64), 0, s, a);
+    hipLaunchKernelGGL((linear4_kernel<KIND, NT, DEPTH>), dim3(grid), dim3(kWaves4 * 64), 0, s, a);
     return hipGetLastError();
 }
 
 template <Kind KIND, int RT>
 hipError_t go_rows(const Linear4Args& a, uint32_t grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((linear4_rows_kernel<KIND, RT>), dim3(grid), dim3(512), rows_lds<RT>(), s, a);
+    hipLaunchKernelGGL((linear4_rows_kernel<KIND, RT>), dim3(grid), dim3(512), (rows_lds<KIND, RT>()), s, a);
     return hipGetLastError();
 }
 
 template <Kind KIND>
 hipError_t choose(const Linear4Args& a, Linear4Shape shape, uint32_t grid, hipStream_t s)
 {
-    if (shape.rt == 1) return shape.nt == 1 ? go<KIND, 1, 1, KIND == kRowsF32 ? 1 : 4>(a, grid, s) : go<KIND, 1, 4, 1>(a, grid, s);
-    if constexpr (KIND == kRowsF32) return go<KIND, 2, 4, 1>(a, grid, s);
+    if (!shape.through_lds) return shape.nt == 1 ? go<KIND, 1, KIND == kRowsF32 ? 1 : 4>(a, grid, s) : go<KIND, 4, 1>(a, grid, s);
+    if constexpr (KIND == kRowsF32) return go_rows<KIND, 1>(a, grid, s);
     else return shape.rt == 2 ? go_rows<KIND, 2>(a, grid, s) : go_rows<KIND, 4>(a, grid, s);
 }
 
 template <Kind KIND, int RT>
-hipError_t prepare_rows() { return hipFuncSetAttribute((const void*)linear4_rows_kernel<KIND, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, rows_lds<RT>()); }
+hipError_t prepare_rows() { return hipFuncSetAttribute((const void*)linear4_rows_kernel<KIND, RT>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)rows_lds<KIND, RT>()); }
 
 }  // namespace
 
-Linear4Shape linear4_shape(uint64_t tiles, uint32_t, uint32_t most_rows, uint32_t n_cus, uint32_t x_dtype)
+// Kernel times (us) of the three forms, 16 x 16 tiles with a workgroup for 16 outputs / for 64 / rows through LDS:
+//   bf16, 24 rows through 4864 x 832 8.5 / 8.7 / 12.8, three tenants of them 14.2 / 9.6 / 13.6; 64 rows through 4096 x 4096 18.6 / 8.7 / 18.5, two tenants
+//   35.6 / 13.7 / 19.0, four 67.5 / 24.4 / 20.6; 40 tenants of 64 rows through 448 x 960 85 / 19.6 / 20.5; one row through 4096 x 8192 6.1 / 7.2, x 32768 16.5 / 13.1
+//   fp32, 64 rows through 4096 x 4096 40.9 / 18.1 / 19.9, two tenants 76.2 / 34.6 / 21.8; 8 tenants of 64 rows through 1024 x 1024 24.2 / 15.1 / 9.6; one row
+//   through 4096 x 32768 64.6 / 31.0 / 21.7
+// So rows go through LDS where that makes half as many workgroups as there are compute units (fp32, whose every value is split: three quarters, and for few
+// rows too) of two k tiles or more to a wave; else a workgroup takes 64 outputs where that makes one for every compute unit, or for every fourth where several rows are read.
+Linear4Shape linear4_shape(uint64_t row_tiles, uint32_t most_rows, uint32_t most_k, uint32_t n_cus, uint32_t x_dtype)
 {
+    const bool f32 = x_dtype == MT_F32;
     Linear4Shape s;
-    s.rt = most_rows <= 16 ? 1 : most_rows <= 32 || x_dtype == MT_F32 ? 2 : 4;
-    s.nt = s.rt > 1 ? (x_dtype == MT_F32 ? 4 : kNt * kSlabs) : tiles >= 16 * (uint64_t)n_cus ? 4 : 1;
+    s.rt = most_rows <= 16 || f32 ? 1 : most_rows <= 32 ? 2 : 4;
+    s.nt = kNt * kSlabs;
+    s.through_lds = (f32 || most_rows > 16) && row_tiles / (s.nt * s.rt) >= (f32 ? 3 * n_cus / 4 : n_cus / 2) && most_k >= 2 * kQuarters * kTile4K;
+    if (!s.through_lds) {
+        s.rt = 1;
+        s.nt = row_tiles / 4 >= (most_rows > 4 ? n_cus / 4 : n_cus) ? 4 : 1;
+    }
     return s;
 }
 
 hipError_t prepare_linear4()
 {
-    hipError_t e = prepare_rows<kRowsBf16, 2>();
+    hipError_t e = prepare_rows<kRowsF32, 1>();
+    if (e == hipSuccess) e = prepare_rows<kRowsBf16, 2>();
     if (e == hipSuccess) e = prepare_rows<kRowsBf16, 4>();
     if (e == hipSuccess) e = prepare_rows<kRowsMx8, 2>();
     return e == hipSuccess ? prepare_rows<kRowsMx8, 4>() : e;

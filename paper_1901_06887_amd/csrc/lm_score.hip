@@ -267,18 +267,18 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
             for (uint32_t g = 0; g < a.n_given; ++g) {
                 const float at = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, given_x), g));
                 const uint32_t c = (uint32_t)__builtin_amdgcn_readlane(given, g);
-                uint32_t count = 0;
+                uint32_t count = 0;               // of this lane
                 if (c < base) {
 #pragma unroll
-                    for (uint32_t i = 0; i < kPer; ++i) count += (uint32_t)__popcll(__ballot(v[i] > at));
+                    for (uint32_t i = 0; i < kPer; ++i) count += v[i] > at;
                 } else if (c >= base + kChunk) {
 #pragma unroll
-                    for (uint32_t i = 0; i < kPer; ++i) count += (uint32_t)__popcll(__ballot(v[i] >= at));
+                    for (uint32_t i = 0; i < kPer; ++i) count += v[i] >= at;
                 } else {
 #pragma unroll
-                    for (uint32_t i = 0; i < kPer; ++i)
-                        count += (uint32_t)__popcll(__ballot(v[i] > at || (v[i] == at && Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec < c)));
+                    for (uint32_t i = 0; i < kPer; ++i) count += v[i] > at || (v[i] == at && Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec < c);
                 }
+                count = wave_total(count);
                 if (lane == g) w.in_front += count;
             }
         if constexpr (TOP) {

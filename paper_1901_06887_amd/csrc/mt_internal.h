@@ -348,8 +348,8 @@ struct ScoreArgs {
     uint32_t parts, part_len;        // workgroups that share a row, and classes of one of them
 };
 hipError_t launch_norm(const mt_norm_args& a, hipStream_t s);
-struct Linear4Shape { uint32_t rt, nt; };      // tiles of 16 rows and of 16 outputs that a workgroup serves
-Linear4Shape linear4_shape(uint64_t tiles, uint32_t k_tiles, uint32_t most_rows, uint32_t n_cus, uint32_t x_dtype);
+struct Linear4Shape { uint32_t rt, nt; bool through_lds; };      // tiles of 16 rows and of 16 outputs that a workgroup serves, and how it takes its rows
+Linear4Shape linear4_shape(uint64_t row_tiles, uint32_t most_rows, uint32_t most_k, uint32_t n_cus, uint32_t x_dtype);      // row_tiles: of 16 outputs x 16 rows
 hipError_t prepare_linear4();      // once per device, before the first launch: lets kernels ask for more than 64 KiB of LDS
 hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s);
 void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len);
