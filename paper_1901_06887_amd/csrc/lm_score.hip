@@ -4,9 +4,10 @@
 // terms that are not negative.  (x - m) / 2 is what is worked with: x - m itself can leave fp32's range.  Every lane carries its own m, S and U and
 // rescales them once per 16 classes; lanes, waves and workgroups are joined at the end.
 //
-// Alternatives: every wave keeps a list in LDS of what can still be among the best `top` of its classes.  Its first 1024 classes set a bar: the
-// top-th largest of the lanes' maxima, which at least `top` of them reach and few others do.  Later classes are in lane order behind those, so an equal
-// one never gets in; a list that fills up is cut to its best `top` and raises the bar.  One comparison a lane and 16 classes is what that costs where nothing passes.
+// Alternatives: every wave keeps a list in LDS of what can still be among the best `top` of its classes.  The waves' first 1024 classes set a bar for all of
+// them: a value that a quarter of `top` lanes' maxima reach in every wave, so that at least `top` classes do, and few others.  Later classes of a wave
+// are in order behind those, so an equal one never gets in; a list that fills up is cut to its best `top` and raises the bar.  One comparison a lane and 16
+// classes is what that costs where nothing passes.
 #include "lm_device.h"
 
 namespace mt {
@@ -14,8 +15,7 @@ namespace {
 
 constexpr float kNone = -__builtin_inff();
 constexpr float kLowest = -3.402823466e38f;
-constexpr uint32_t kPer = 16;                     // classes of a lane at a time
-constexpr uint32_t kChunk = 64 * kPer;            // ... of a wave
+constexpr uint32_t kSome = 1024;                  // classes that are enough for a wave
 constexpr uint32_t kList = 192;                   // entries of a wave's list
 constexpr uint32_t kWaves = 4;                    // waves of a workgroup
 constexpr uint32_t kSplitRows = 1024;             // most rows whose classes workgroups share
@@ -102,6 +102,7 @@ struct List {
     uint32_t n;
     float bar, equal;
     __device__ __forceinline__ bool keeps(float x) const { return x > bar || x == equal; }
+    __device__ __forceinline__ void raise(float to) { if (to > bar) equal = bar = to; }
 
     // Leaves the best `top` of the entries, in order, and raises the bar to the last of them.
     __device__ __forceinline__ void cut(uint32_t top, uint32_t lane)
@@ -132,26 +133,31 @@ struct List {
 };
 constexpr uint32_t kListRoom = kList - 64;        // entries up to which every lane can still append one
 
-// The top-th largest of the lanes' values, rounded down a little; -infinity if there are not so many.
-__device__ __forceinline__ float bar_of(float v, uint32_t top)
+// A value that at least n of the lanes' values reach, and not many more; -infinity if there are not so many.
+__device__ __forceinline__ float bar_of(float v, uint32_t n)
 {
-    // by bits from the highest, over values ordered as integers; 16 of them decide
+    // between the smallest and the largest, over values ordered as integers, an eighth at a time: three rounds of seven comparisons that wait for nothing
+    // between them (bit by bit, sixteen that each wait for a count, took three times as long)
     uint32_t b = __builtin_bit_cast(uint32_t, v);
-    b = v == kNone ? 0 : b & 0x80000000u ? ~b : b | 0x80000000u;
-    uint32_t found = 0;
+    b = v > kNone ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0;
+    if ((uint32_t)__popcll(__ballot(b != 0)) < n) return kNone;
+    uint32_t lo = ~wave_fold(b ? ~b : 0u, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+    uint32_t span = wave_fold(b, [](uint32_t p, uint32_t q) { return p > q ? p : q; }) - lo;
 #pragma nounroll
-    for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t probe = found | 1u << bit;
-        if ((uint32_t)__popcll(__ballot(b >= probe)) >= top) found = probe;
+    for (int round = 0; round < 3; ++round) {
+        const uint32_t step = span / 8 + 1;
+        uint32_t eighths = 0;
+#pragma unroll
+        for (uint32_t i = 1; i < 8; ++i) eighths += (uint32_t)__popcll(__ballot(b >= lo + i * step)) >= n;
+        lo += eighths * step;
+        span = step;
     }
-    if (found == 0) return kNone;
-    const float bar = __builtin_bit_cast(float, found & 0x80000000u ? found ^ 0x80000000u : ~found);
-    return bar == bar ? bar : kNone;              // (bits of a NaN below all numbers: not so many of them)
+    return __builtin_bit_cast(float, lo & 0x80000000u ? lo ^ 0x80000000u : ~lo);
 }
 
 // A lane's 16 classes of a chunk as they come from memory: vectors of 16 bytes, 64 of them side by side.
 template <typename T> struct Raw {
-    static constexpr uint32_t kVec = 16 / sizeof(T), kVecs = kPer / kVec;
+    static constexpr uint32_t kVec = 16 / sizeof(T), kVecs = 4, kPer = kVec * kVecs, kChunk = 64 * kPer;      // ... a lane's and a wave's classes at a time
     u32x4 v[kVecs];
     uint32_t bits[kVecs];
 
@@ -215,6 +221,25 @@ template <typename T> struct Raw {
     }
 };
 
+// The same for the lanes of all the waves: n values at least reach it.  (Where a wave alone has too few, what n in some other wave reach.)
+template <uint32_t WAVES>
+__device__ __forceinline__ float bar_of_all(float v, uint32_t n, float* lds, uint32_t wave)
+{
+    if constexpr (WAVES == 1) return bar_of(v, n);
+    float bar = kNone;
+#pragma nounroll
+    for (int all = 1; all >= 0 && bar == kNone; --all) {
+        const float mine = bar_of(v, all ? (n + WAVES - 1) / WAVES : n);
+        __syncthreads();
+        lds[wave] = mine;
+        __syncthreads();
+        bar = lds[0];
+#pragma unroll
+        for (uint32_t w = 1; w < WAVES; ++w) bar = all ? fminf(bar, lds[w]) : fmaxf(bar, lds[w]);
+    }
+    return bar;
+}
+
 // Everything that a wave, then a workgroup, knows of its share of a row.
 struct Share {
     Sums sums;
@@ -223,8 +248,9 @@ struct Share {
 
 // WAVES waves share a row's part [blockIdx.y]; WAVES 1: every wave of the workgroup has a row of its own.
 template <typename T, bool TOP, bool MASK, uint32_t WAVES>
-__global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
+__global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
 {
+    constexpr uint32_t kPer = Raw<T>::kPer, kChunk = Raw<T>::kChunk;
     const mt_score_args& a = s.a;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t row = WAVES == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
@@ -238,7 +264,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
     const uint32_t wave_len = WAVES == 1 ? s.part_len : ceil_div(s.part_len, WAVES * kChunk) * kChunk;
     uint32_t base = part * s.part_len + (WAVES == 1 ? 0 : wave * wave_len);
     const uint32_t mem_end = base < part_end ? min((uint64_t)base + wave_len, (uint64_t)part_end) : base;      // this wave's classes, and no more are read
-    Raw<T> raw;
+    Raw<T> raw{};
     if (base < mem_end) raw.template load<MASK>(x, allowed, base, lane, mem_end);
     const uint32_t n = a.n_classes ? (uint32_t)min(max(a.n_classes[row], 0), (int32_t)a.classes) : a.classes;
     const uint32_t end = min(mem_end, n);
@@ -248,7 +274,10 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
 
     Share w{{kLowest, 0.0f, 0.0f}, 0};
     List list{TOP ? lists[wave] : nullptr, TOP ? best[wave] : nullptr, 0, kNone, __builtin_nanf("")};
-    for (; base < end; base += kChunk) {
+    __shared__ float wave_bars[WAVES];
+    uint32_t first_in_front = 0;      // of given class 0, by this lane's classes
+    // (the first time round also without a class: all waves set the bar together)
+    for (bool first = true; first || base < end; base += kChunk, first = false) {
         float v[kPer];
         raw.template logits<MASK>(v, base, lane, end);
         if (base + kChunk < end) raw.template load<MASK>(x, allowed, base + kChunk, lane, mem_end);
@@ -278,16 +307,19 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
 #pragma unroll
                     for (uint32_t i = 0; i < kPer; ++i) count += v[i] > at || (v[i] == at && Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec < c);
                 }
-                count = wave_total(count);
-                if (lane == g) w.in_front += count;
+                if (g == 0) first_in_front += count;
+                else {
+                    count = wave_total(count);
+                    if (lane == g) w.in_front += count;
+                }
             }
         if constexpr (TOP) {
             list.equal = __builtin_nanf("");      // what is in the list is in front of an equal class of this chunk
-            const uint64_t lanes = __ballot(most > list.bar);
+            if (first) list.raise(bar_of_all<WAVES>(most, a.top, wave_bars, wave));
+            const uint64_t lanes = __ballot(most > list.bar || most == list.equal);
             if (lanes) {
-                if ((uint32_t)__popcll(lanes) >= a.top) {
-                    const float bar = bar_of(most, a.top);
-                    if (bar > list.bar) list.equal = list.bar = bar;
+                if (!first && (uint32_t)__popcll(lanes) >= a.top) {
+                    list.raise(bar_of(most, a.top));
                 }
                 uint32_t mine = 0;
 #pragma unroll
@@ -305,6 +337,8 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
             }
         }
     }
+    first_in_front = wave_total(first_in_front);
+    if (lane == 0) w.in_front += first_in_front;
     w.sums.over_wave(s.exp2_scale);
     // The waves' shares to wave 0, the entries of all lists to their places; then, in a row of several parts, the same with what they handed over.
     __shared__ Sums wave_sums[WAVES];
@@ -318,7 +352,11 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
         } else wave_sync();
         uint32_t n = list.n;
         if constexpr (TOP) {
-            if constexpr (WAVES > 1) n = wave_n[0] + wave_n[1] + wave_n[2] + wave_n[3];
+            if constexpr (WAVES > 1) {
+                n = 0;
+#pragma unroll
+                for (uint32_t o = 0; o < WAVES; ++o) n += wave_n[o];
+            }
             n = min(n, a.top);
 #pragma nounroll
             for (uint32_t j = 0; j < list.n; j += 64) {
@@ -381,11 +419,11 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
                 }
             w.sums.over_wave(s.exp2_scale);
             if constexpr (TOP) {
-                list.n = 0; list.bar = kNone;
+                list.n = 0; list.bar = kNone; list.equal = __builtin_nanf("");
                 float most = kNone;
 #pragma unroll
                 for (uint32_t j = 0; j < kPartKeys; ++j) if (keys[j]) most = fmaxf(most, key_logit(keys[j]));
-                list.equal = list.bar = bar_of(most, a.top);
+                list.raise(bar_of_all<WAVES>(most, a.top, wave_bars, wave));
 #pragma nounroll
                 for (uint32_t j = 0; j * 64 < mine * a.top; ++j) {
                     uint64_t one = keys[0];
@@ -423,10 +461,12 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreArgs s)
 template <typename T, bool TOP, bool MASK>
 hipError_t go(const ScoreArgs& s, hipStream_t st)
 {
-    if (s.parts == 1 && s.a.classes <= 2 * kChunk)
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(256), 0, st, s);
+    // A wave to a row where rows are short, or many for their length (us, four waves / one, 5 alternatives, fp32 and bf16: 256 rows of 4000 classes 8.2 / 11.7 and
+    // 9.8 / 10.3, 1024 rows 12.8 / 13.5 and 14.1 / 11.5; 2048 rows of 4000 19.9 / 15.7 and 24.5 / 13.8, of 8192 27.0 / 23.1 and 24.8 / 18.6, of 32768 67 / 75 and 54 / 53).
+    if (s.parts == 1 && (s.a.classes <= 2 * kSome || (s.a.classes <= 8 * kSome && s.a.classes <= 4 * (uint64_t)s.a.rows)))
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(64 * kWaves), 0, st, s);
     else
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves>), dim3(s.a.rows, s.parts), dim3(256), 0, st, s);
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves>), dim3(s.a.rows, s.parts), dim3(64 * kWaves), 0, st, s);
     return hipGetLastError();
 }
 
@@ -447,7 +487,7 @@ void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* par
 {
     *parts = 1; *part_len = classes;
     if (rows == 0 || rows > kSplitRows / 2) return;
-    const uint32_t span = kChunk * kWaves, want = std::min(kMaxParts, kSplitRows / rows);
+    const uint32_t span = kSome * kWaves, want = std::min(kMaxParts, kSplitRows / rows);
     const uint32_t spans = (classes + span - 1) / span;
     if (spans < 3 || want < 3) return;
     *part_len = (spans + want - 1) / want * span;
