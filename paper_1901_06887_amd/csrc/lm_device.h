@@ -34,17 +34,21 @@ __device__ __forceinline__ void load8(const float* p, float (&v)[8])
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
 }
-__device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
+// ... and back, STREAM: past the caches (nothing reads them before they are full of later rows).
+template <bool STREAM> __device__ __forceinline__ void store8(__bf16* p, const float (&v)[8])
 {
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-    *(Any<__bf16>::vec16*)p = w;
+    if constexpr (STREAM) __builtin_nontemporal_store(w, (Any<__bf16>::vec16*)p); else *(Any<__bf16>::vec16*)p = w;
 }
-__device__ __forceinline__ void store8(float* p, const float (&v)[8])
+template <bool STREAM> __device__ __forceinline__ void store8(float* p, const float (&v)[8])
 {
     const f32x4 a = {v[0], v[1], v[2], v[3]}, b = {v[4], v[5], v[6], v[7]};
-    *(Any<float>::vec16*)p = __builtin_bit_cast(u32x4, a); *(Any<float>::vec16*)(p + 4) = __builtin_bit_cast(u32x4, b);
+    const u32x4 wa = __builtin_bit_cast(u32x4, a), wb = __builtin_bit_cast(u32x4, b);
+    Any<float>::vec16 *qa = (Any<float>::vec16*)p, *qb = (Any<float>::vec16*)(p + 4);
+    if constexpr (STREAM) { __builtin_nontemporal_store(wa, qa); __builtin_nontemporal_store(wb, qb); }
+    else { *qa = wa; *qb = wb; }
 }
 // The first n (0 .. 8) of them, element by element; zeros behind.
 template <typename T> __device__ __forceinline__ void load_some(const T* p, uint32_t n, float (&v)[8])

@@ -2,13 +2,16 @@
 //
 // h = x + r, y = h * rsqrt(mean(h^2) + eps) * gain, q = e4m3(y / 2^e) with the least e >= -126 for which no |y| of the
 // 32 values exceeds 448 * 2^e.  A row is read once and stays in registers between the sum of squares and the outputs; a lane
-// holds runs of eight consecutive elements, so a block of 32 is four neighbouring lanes and its maximum two cross-lane moves.
+// holds runs of eight consecutive elements, so a block of 32 is four neighbouring lanes and its maximum two cross-lane moves.  Memory bounds it: 8192 rows of
+// 4096 bf16, residual, sum, norm and 8-bit rows 53.8 us, 5.6 TB/s.  One row of 1024 takes 2.6 us, which is the launch and one trip to memory.
 #include "lm_device.h"
 
 namespace mt {
 namespace {
 
 constexpr uint32_t kRun = 8;                  // consecutive elements of a lane
+// Outputs of more than what the L2s hold (8 x 4 MiB) go past them: 8192 rows of 4096 bf16, sum, norm and 8-bit rows, 65.5 -> 59.7 us, of 2048 30.0 -> 22.7.
+constexpr uint64_t kStreamBytes = 32ull << 20;
 
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
@@ -70,7 +73,7 @@ __device__ __forceinline__ void load_run(const NormRow<T>& r, uint32_t at, uint3
 }
 
 // Everything behind the mean: the run's sum, norm and 8-bit values.  All lanes of a block come here together.
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uint32_t width, const float (&h)[kRun], float scale)
 {
     const uint32_t n = at >= width ? 0 : width - at < kRun ? width - at : kRun;
@@ -84,8 +87,8 @@ __device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uin
         if (r.gain) y[i] *= g[i];
         if (!r.known || i >= n) y[i] = 0.0f;
     }
-    if (r.sum && n) { if (n == kRun) store8(r.sum + at, h); else store_some(r.sum + at, n, h); }
-    if (r.y && n) { if (n == kRun) store8(r.y + at, y); else store_some(r.y + at, n, y); }
+    if (r.sum && n) { if (n == kRun) store8<STREAM>(r.sum + at, h); else store_some(r.sum + at, n, h); }
+    if (r.y && n) { if (n == kRun) store8<STREAM>(r.y + at, y); else store_some(r.y + at, n, y); }
     if (!r.y8) return;
     // magnitudes as integers: they order like the values, and a NaN stays above every number
     uint32_t most = 0;
@@ -104,73 +107,76 @@ __device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uin
         w = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2] * down, y[4 * i + 3] * down, w, true);
         q[i] = finite ? (uint32_t)w : 0x7f7f7f7fu;
     }
-    if (n == kRun) *(Any<uint8_t>::vec8*)(r.y8 + at) = Any<uint8_t>::vec8{q[0], q[1]};
-    else
+    if (n == kRun) {
+        Any<uint8_t>::vec8* to = (Any<uint8_t>::vec8*)(r.y8 + at);
+        const u32x2 w = {q[0], q[1]};
+        if constexpr (STREAM) __builtin_nontemporal_store(w, to); else *to = w;
+    } else
 #pragma unroll
         for (uint32_t i = 0; i < kRun; ++i) if (i < n) r.y8[at + i] = (uint8_t)(q[i / 4] >> (8 * (i % 4)));
     if (n && at % MT_MX_BLOCK == 0) r.y8_scales[at / MT_MX_BLOCK] = finite ? (uint8_t)(e + 127) : 0xff;
 }
 
-// THREADS to a row, each with RUNS runs of it in registers (run j of thread t at (j * THREADS + t) * 8); WGS rows to a workgroup
-// of one wave each where THREADS is 64.  LOOP: a row that no workgroup holds is read a second time for the outputs.
-template <typename T, uint32_t THREADS, uint32_t RUNS, bool LOOP>
-__global__ void __launch_bounds__(THREADS == 64 ? 256 : THREADS) norm_kernel(mt_norm_args a)
+// Workgroups of the threads that a row needs (MULTI), or of four waves with a row each.  A thread holds RUNS runs of its row in registers, run j of thread t
+// at (j * threads + t) * 8.  LOOP: a row that no workgroup holds is read a second time for the outputs.  STREAM: outputs past the caches.
+template <typename T, bool MULTI, uint32_t RUNS, bool LOOP, bool STREAM>
+__global__ void __launch_bounds__(MULTI ? 1024 : 256) norm_kernel(mt_norm_args a)
 {
-    constexpr uint32_t kSpan = THREADS * kRun;
-    const uint32_t t = THREADS == 64 ? threadIdx.x & 63 : threadIdx.x;
-    const uint32_t row = THREADS == 64 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
+    const uint32_t threads = MULTI ? blockDim.x : 64, span = threads * kRun;
+    const uint32_t t = MULTI ? threadIdx.x : threadIdx.x & 63;
+    const uint32_t row = MULTI ? blockIdx.x : blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (row >= a.rows) return;                // (whole waves, and only where no barrier follows)
     const NormRow<T> r = norm_row<T>(a, row);
     float h[RUNS][kRun];
     float squares = 0.0f;
-    for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * kSpan) {
+    for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * span) {
 #pragma unroll
-        for (uint32_t j = 0; j < RUNS; ++j) {
-            load_run(r, base + j * kSpan + t * kRun, a.width, h[j]);
-        }
+        for (uint32_t j = 0; j < RUNS; ++j) load_run(r, base + j * span + t * kRun, a.width, h[j]);
 #pragma unroll
         for (uint32_t j = 0; j < RUNS; ++j)
 #pragma unroll
             for (uint32_t i = 0; i < kRun; ++i) squares = fmaf(h[j][i], h[j][i], squares);
     }
     squares = wave_total(squares);
-    if constexpr (THREADS > 64) {
-        __shared__ float part[THREADS / 64];
+    if constexpr (MULTI) {
+        __shared__ float part[16];
         if ((t & 63) == 0) part[t >> 6] = squares;
         __syncthreads();
         squares = 0.0f;
-#pragma unroll
-        for (uint32_t w = 0; w < THREADS / 64; ++w) squares += part[w];
+        for (uint32_t w = 0; w < threads / 64; ++w) squares += part[w];
     }
     const float scale = 1.0f / __builtin_sqrtf(squares / (float)a.width + a.eps);
-    for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * kSpan) {
+    for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * span) {
 #pragma unroll
         for (uint32_t j = 0; j < RUNS; ++j) {
-            const uint32_t at = base + j * kSpan + t * kRun;
+            const uint32_t at = base + j * span + t * kRun;
             if (LOOP) load_run(r, at, a.width, h[j]);
-            finish_run(r, at, a.width, h[j], scale);
+            finish_run<STREAM>(r, at, a.width, h[j], scale);
         }
     }
 }
 
-template <typename T, uint32_t THREADS, uint32_t RUNS, bool LOOP = false>
-hipError_t go(const mt_norm_args& a, hipStream_t s)
+template <typename T, bool MULTI, uint32_t RUNS, bool LOOP = false>
+hipError_t go(const mt_norm_args& a, bool stream, hipStream_t s)
 {
-    const uint32_t grid = THREADS == 64 ? (a.rows + 3) / 4 : a.rows;
-    hipLaunchKernelGGL((norm_kernel<T, THREADS, RUNS, LOOP>), dim3(grid), dim3(THREADS == 64 ? 256 : THREADS), 0, s, a);
+    const uint32_t grid = MULTI ? a.rows : (a.rows + 3) / 4;
+    const uint32_t need = (a.width + kRun * RUNS - 1) / (kRun * RUNS);
+    const uint32_t threads = MULTI ? std::min<uint32_t>((need + 63) / 64 * 64, 1024) : 256;
+    if (stream) hipLaunchKernelGGL((norm_kernel<T, MULTI, RUNS, LOOP, true>), dim3(grid), dim3(threads), 0, s, a);
+    else hipLaunchKernelGGL((norm_kernel<T, MULTI, RUNS, LOOP, false>), dim3(grid), dim3(threads), 0, s, a);
     return hipGetLastError();
 }
 
 template <typename T>
 hipError_t choose(const mt_norm_args& a, hipStream_t s)
 {
-    if (a.width <= 512) return go<T, 64, 1>(a, s);
-    if (a.width <= 1024) return go<T, 64, 2>(a, s);
-    if (a.width <= 2048) return go<T, 256, 1>(a, s);
-    if (a.width <= 4096) return go<T, 256, 2>(a, s);
-    if (a.width <= 8192) return go<T, 256, 4>(a, s);
-    if (a.width <= 16384) return go<T, 1024, 2>(a, s);
-    return go<T, 1024, 2, true>(a, s);
+    const uint64_t outputs = (uint64_t)a.rows * a.width * ((a.sum ? sizeof(T) : 0) + (a.y ? sizeof(T) : 0) + (a.y8 ? 1 : 0));
+    const bool stream = outputs > kStreamBytes;
+    // (one run a thread: with two, 8192 rows of 4096 take 58.5 us instead of 53.8, one row of 4096 3.7 instead of 2.8)
+    if (a.width <= 512) return go<T, false, 1>(a, stream, s);
+    if (a.width <= 8192) return go<T, true, 1>(a, stream, s);
+    if (a.width <= 16384) return go<T, true, 2>(a, stream, s);
+    return go<T, true, 2, true>(a, stream, s);
 }
 
 }  // namespace
