@@ -18,7 +18,7 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr uint32_t kSome = 1024;                  // classes that are enough for a wave
 constexpr uint32_t kList = 192;                   // entries of a wave's list
 constexpr uint32_t kWaves = 4;                    // waves of a workgroup
-constexpr uint32_t kSplitRows = 1024;             // most rows whose classes workgroups share
+constexpr uint32_t kRecords = 1024;               // most rows x parts where workgroups share a row's classes
 constexpr uint32_t kMaxParts = 64;                // most workgroups that share one
 constexpr uint32_t kPartKeys = kMaxParts / kWaves * MT_SCORE_MAX_TOP / 64;      // keys of a lane where parts are joined
 
@@ -156,8 +156,8 @@ __device__ __forceinline__ float bar_of(float v, uint32_t n)
 }
 
 // A lane's 16 classes of a chunk as they come from memory: vectors of 16 bytes, 64 of them side by side.
-template <typename T> struct Raw {
-    static constexpr uint32_t kVec = 16 / sizeof(T), kVecs = 4, kPer = kVec * kVecs, kChunk = 64 * kPer;      // ... a lane's and a wave's classes at a time
+template <typename T, uint32_t VECS> struct Raw {
+    static constexpr uint32_t kVec = 16 / sizeof(T), kVecs = VECS, kPer = kVec * kVecs, kChunk = 64 * kPer;      // ... a lane's and a wave's classes at a time
     u32x4 v[kVecs];
     uint32_t bits[kVecs];
 
@@ -247,10 +247,12 @@ struct Share {
 };
 
 // WAVES waves share a row's part [blockIdx.y]; WAVES 1: every wave of the workgroup has a row of its own.
-template <typename T, bool TOP, bool MASK, uint32_t WAVES>
-__global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
+template <typename T, bool TOP, bool MASK, uint32_t WAVES, bool PARTS>
+__global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
 {
-    constexpr uint32_t kPer = Raw<T>::kPer, kChunk = Raw<T>::kChunk;
+    // (four vectors keep the memory busy: 2048 rows of 32768 bf16 classes 54 -> 50 us; where the row is shared they would leave waves without classes)
+    using R = Raw<T, PARTS && sizeof(T) == 2 ? 2 : 4>;
+    constexpr uint32_t kPer = R::kPer, kChunk = R::kChunk;
     const mt_score_args& a = s.a;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t row = WAVES == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
@@ -259,12 +261,12 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
     __shared__ __attribute__((aligned(16))) uint64_t best[TOP ? kWaves : 1][TOP ? MT_SCORE_MAX_TOP : 1];
     const T* x = (const T*)a.logits + row * a.row_stride;
     const uint32_t* allowed = MASK ? a.allowed + row * a.allowed_stride : nullptr;
-    const uint32_t part = WAVES == 1 ? 0 : blockIdx.y;
+    const uint32_t part = PARTS ? blockIdx.y : 0;
     const uint32_t part_end = min((uint64_t)(part + 1) * s.part_len, (uint64_t)a.classes);
     const uint32_t wave_len = WAVES == 1 ? s.part_len : ceil_div(s.part_len, WAVES * kChunk) * kChunk;
     uint32_t base = part * s.part_len + (WAVES == 1 ? 0 : wave * wave_len);
     const uint32_t mem_end = base < part_end ? min((uint64_t)base + wave_len, (uint64_t)part_end) : base;      // this wave's classes, and no more are read
-    Raw<T> raw{};
+    R raw{};
     if (base < mem_end) raw.template load<MASK>(x, allowed, base, lane, mem_end);
     const uint32_t n = a.n_classes ? (uint32_t)min(max(a.n_classes[row], 0), (int32_t)a.classes) : a.classes;
     const uint32_t end = min(mem_end, n);
@@ -305,7 +307,7 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
                     for (uint32_t i = 0; i < kPer; ++i) count += v[i] >= at;
                 } else {
 #pragma unroll
-                    for (uint32_t i = 0; i < kPer; ++i) count += v[i] > at || (v[i] == at && Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec < c);
+                    for (uint32_t i = 0; i < kPer; ++i) count += v[i] > at || (v[i] == at && R::first(base, i / R::kVec, lane) + i % R::kVec < c);
                 }
                 if (g == 0) first_in_front += count;
                 else {
@@ -331,7 +333,7 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
 #pragma unroll
                     for (uint32_t j = 1; j < kPer; ++j) one = i == j ? v[j] : one;
                     if (list.n > kListRoom) list.cut(a.top, lane);
-                    list.append(mine != 0 && list.keeps(one), order_key(one, Raw<T>::first(base, i / Raw<T>::kVec, lane) + i % Raw<T>::kVec));
+                    list.append(mine != 0 && list.keeps(one), order_key(one, R::first(base, i / R::kVec, lane) + i % R::kVec));
                     mine &= mine - 1;
                 }
             }
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
     // The waves' shares to wave 0, the entries of all lists to their places; then, in a row of several parts, the same with what they handed over.
     __shared__ Sums wave_sums[WAVES];
     __shared__ uint32_t wave_n[WAVES], wave_front[WAVES][MT_SCORE_MAX_GIVEN], last;
-    for (bool parts_joined = s.parts == 1;; parts_joined = true) {
+    for (bool parts_joined = !PARTS;; parts_joined = true) {
         if constexpr (TOP) if (lane < kStep) list.at[list.n + lane] = 0;
         if constexpr (WAVES > 1) {
             if (lane == 0) { wave_sums[wave] = w.sums; wave_n[wave] = list.n; }
@@ -383,10 +385,10 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(ScoreArgs s)
         }
         list.n = n;
         if (parts_joined) break;
-        if constexpr (WAVES > 1) {
+        if constexpr (PARTS) {
             // the last workgroup of a row to come here joins the parts of all of them
             uint32_t* tickets = (uint32_t*)a.scratch;
-            Part* parts = (Part*)((uint8_t*)a.scratch + kSplitRows * 4) + (uint64_t)row * s.parts;
+            Part* parts = (Part*)((uint8_t*)a.scratch + kRecords * 4) + (uint64_t)row * s.parts;
             if (wave == 0) {
                 Part& p = parts[part];
                 if (lane == 0) { hand_over(&p.m, w.sums.m); hand_over(&p.s, w.sums.s); hand_over(&p.u, w.sums.u); }
@@ -464,9 +466,11 @@ hipError_t go(const ScoreArgs& s, hipStream_t st)
     // A wave to a row where rows are short, or many for their length (us, four waves / one, 5 alternatives, fp32 and bf16: 256 rows of 4000 classes 8.2 / 11.7 and
     // 9.8 / 10.3, 1024 rows 12.8 / 13.5 and 14.1 / 11.5; 2048 rows of 4000 19.9 / 15.7 and 24.5 / 13.8, of 8192 27.0 / 23.1 and 24.8 / 18.6, of 32768 67 / 75 and 54 / 53).
     if (s.parts == 1 && (s.a.classes <= 2 * kSome || (s.a.classes <= 8 * kSome && s.a.classes <= 4 * (uint64_t)s.a.rows)))
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(64 * kWaves), 0, st, s);
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(64 * kWaves), 0, st, s);
+    else if (s.parts == 1)
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false>), dim3(s.a.rows), dim3(64 * kWaves), 0, st, s);
     else
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves>), dim3(s.a.rows, s.parts), dim3(64 * kWaves), 0, st, s);
+        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, true>), dim3(s.a.rows, s.parts), dim3(64 * kWaves), 0, st, s);
     return hipGetLastError();
 }
 
@@ -486,9 +490,8 @@ hipError_t choose(const ScoreArgs& s, hipStream_t st)
 void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len)
 {
     *parts = 1; *part_len = classes;
-    if (rows == 0 || rows > kSplitRows / 2) return;
-    const uint32_t span = kSome * kWaves, want = std::min(kMaxParts, kSplitRows / rows);
-    const uint32_t spans = (classes + span - 1) / span;
+    if (rows == 0) return;
+    const uint32_t span = kSome * kWaves, spans = (classes + span - 1) / span, want = std::min(kMaxParts, kRecords / rows);
     if (spans < 3 || want < 3) return;
     *part_len = (spans + want - 1) / want * span;
     *parts = (uint32_t)(((uint64_t)classes + *part_len - 1) / *part_len);
@@ -499,7 +502,7 @@ uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t, uint32_t
 {
     uint32_t parts, part_len;
     score_split(rows, classes, &parts, &part_len);
-    return parts > 1 ? kSplitRows * (4 + sizeof(Part)) : 0;      // rows x parts is never more than that
+    return parts > 1 ? kRecords * (4 + sizeof(Part)) : 0;
 }
 
 hipError_t launch_score(const ScoreArgs& a, hipStream_t s)
