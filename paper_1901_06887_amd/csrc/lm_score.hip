@@ -94,15 +94,18 @@ __device__ __forceinline__ uint32_t in_front_of(uint64_t key, const uint64_t* at
     return n;
 }
 
-// Entries of a wave's list in no order, and the bar: a class is kept if its logit is above `bar`, or equal to `equal` (NaN: to nothing).
+// Entries of a wave's list in no order, and the bar: a class is kept if its logit is above it.  A bar raised to a value lies a little below it for the rest
+// of the chunk, whose classes equal to it may come in front of some in the list, and at the value from the next chunk on.
 // (The code is kept short, in loops: a call runs it once, so much of its time is the fetch of the code.)
 struct List {
     uint64_t* at;         // LDS, kList entries and kStep more
     uint64_t* best;       // LDS, MT_SCORE_MAX_TOP entries
     uint32_t n;
-    float bar, equal;
-    __device__ __forceinline__ bool keeps(float x) const { return x > bar || x == equal; }
-    __device__ __forceinline__ void raise(float to) { if (to > bar) equal = bar = to; }
+    float bar, next;
+    __device__ __forceinline__ void raise(float to)
+    {
+        if (to > next) { next = to; bar = to - fmaf(fabsf(to), 1e-6f, 1.2e-38f); }
+    }
 
     // Leaves the best `top` of the entries, in order, and raises the bar to the last of them.
     __device__ __forceinline__ void cut(uint32_t top, uint32_t lane)
@@ -121,7 +124,7 @@ struct List {
         if (n > top) n = top;
         if (lane < n) at[lane] = best[lane];
         wave_sync();
-        if (n == top) equal = bar = key_logit(at[top - 1]);
+        if (n == top) raise(key_logit(at[top - 1]));
     }
 
     __device__ __forceinline__ void append(bool keep, uint64_t key)
@@ -275,7 +278,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
     const float given_x = given >= 0 ? logit(x, allowed, (uint32_t)given, n) : kNone;
 
     Share w{{kLowest, 0.0f, 0.0f}, 0};
-    List list{TOP ? lists[wave] : nullptr, TOP ? best[wave] : nullptr, 0, kNone, __builtin_nanf("")};
+    List list{TOP ? lists[wave] : nullptr, TOP ? best[wave] : nullptr, 0, kNone, kNone};
     __shared__ float wave_bars[WAVES];
     uint32_t first_in_front = 0;      // of given class 0, by this lane's classes
     // (the first time round also without a class: all waves set the bar together)
@@ -316,16 +319,19 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
                 }
             }
         if constexpr (TOP) {
-            list.equal = __builtin_nanf("");      // what is in the list is in front of an equal class of this chunk
+            list.bar = list.next;
             if (first) list.raise(bar_of_all<WAVES>(most, a.top, wave_bars, wave));
-            const uint64_t lanes = __ballot(most > list.bar || most == list.equal);
+            const uint64_t lanes = __ballot(most > list.bar);
             if (lanes) {
-                if (!first && (uint32_t)__popcll(lanes) >= a.top) {
-                    list.raise(bar_of(most, a.top));
-                }
+                if (!first && (uint32_t)__popcll(lanes) >= a.top) list.raise(bar_of(most, a.top));
                 uint32_t mine = 0;
 #pragma unroll
-                for (uint32_t i = 0; i < kPer; ++i) mine |= list.keeps(v[i]) ? 1u << i : 0;
+                for (uint32_t i = 0; i < kPer; ++i) mine |= v[i] > list.bar ? 1u << i : 0;
+                if (list.n <= kListRoom && !__ballot((mine & (mine - 1)) != 0)) {       // mostly: one of a lane's at most, its largest
+                    const uint32_t i = mine ? __builtin_ctz(mine) : 0;
+                    list.append(mine != 0, order_key(most, R::first(base, i / R::kVec, lane) + i % R::kVec));
+                    mine = 0;
+                }
 #pragma nounroll
                 while (__ballot(mine != 0)) {
                     const uint32_t i = mine ? __builtin_ctz(mine) : 0;
@@ -333,7 +339,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
 #pragma unroll
                     for (uint32_t j = 1; j < kPer; ++j) one = i == j ? v[j] : one;
                     if (list.n > kListRoom) list.cut(a.top, lane);
-                    list.append(mine != 0 && list.keeps(one), order_key(one, R::first(base, i / R::kVec, lane) + i % R::kVec));
+                    list.append(mine != 0 && one > list.bar, order_key(one, R::first(base, i / R::kVec, lane) + i % R::kVec));
                     mine &= mine - 1;
                 }
             }
@@ -421,7 +427,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
                 }
             w.sums.over_wave(s.exp2_scale);
             if constexpr (TOP) {
-                list.n = 0; list.bar = kNone; list.equal = __builtin_nanf("");
+                list.n = 0; list.bar = list.next = kNone;
                 float most = kNone;
 #pragma unroll
                 for (uint32_t j = 0; j < kPartKeys; ++j) if (keys[j]) most = fmaxf(most, key_logit(keys[j]));
@@ -432,7 +438,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
 #pragma unroll
                     for (uint32_t k = 1; k < kPartKeys; ++k) one = j == k ? keys[k] : one;
                     if (list.n > kListRoom) list.cut(a.top, lane);
-                    list.append(one && list.keeps(key_logit(one)), one);
+                    list.append(one && key_logit(one) > list.bar, one);
                 }
                 __syncthreads();                  // (the lists and `best` are read no more)
             }
