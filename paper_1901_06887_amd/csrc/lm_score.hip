@@ -5,9 +5,9 @@
 // rescales them once per 16 classes; lanes, waves and workgroups are joined at the end.
 //
 // Alternatives: every wave keeps a list in LDS of what can still be among the best `top` of its classes.  The waves' first 1024 classes set a bar for all of
-// them: a value that a quarter of `top` lanes' maxima reach in every wave, so that at least `top` classes do, and few others.  Later classes of a wave
-// are in order behind those, so an equal one never gets in; a list that fills up is cut to its best `top` and raises the bar.  One comparison a lane and 16
-// classes is what that costs where nothing passes.
+// them: a value that a quarter of `top` lanes' maxima reach in every wave, so that at least `top` classes do, and few others.  What a wave has in its own
+// list is in order in front of its later classes, so of those an equal one doesn't get in; a list that fills up is cut to its best `top` and raises the bar.
+// One comparison a lane and 16 classes is what that costs where nothing passes.
 #include "lm_device.h"
 
 namespace mt {
@@ -94,6 +94,9 @@ __device__ __forceinline__ uint32_t in_front_of(uint64_t key, const uint64_t* at
     return n;
 }
 
+// A value a little below: what is equal to x is above it.
+__device__ __forceinline__ float below(float x) { return x - fmaf(fabsf(x), 1e-6f, 1.2e-38f); }
+
 // Entries of a wave's list in no order, and the bar: a class is kept if its logit is above it.  A bar raised to a value lies a little below it for the rest
 // of the chunk, whose classes equal to it may come in front of some in the list, and at the value from the next chunk on.
 // (The code is kept short, in loops: a call runs it once, so much of its time is the fetch of the code.)
@@ -104,7 +107,7 @@ struct List {
     float bar, next;
     __device__ __forceinline__ void raise(float to)
     {
-        if (to > next) { next = to; bar = to - fmaf(fabsf(to), 1e-6f, 1.2e-38f); }
+        if (to > next) { next = to; bar = below(to); }
     }
 
     // Leaves the best `top` of the entries, in order, and raises the bar to the last of them.
@@ -320,7 +323,11 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
             }
         if constexpr (TOP) {
             list.bar = list.next;
-            if (first) list.raise(bar_of_all<WAVES>(most, a.top, wave_bars, wave));
+            if (first) {
+                // (classes of other waves that reach it come behind this wave's next chunk: an equal one there has to get in)
+                const float all = bar_of_all<WAVES>(most, a.top, wave_bars, wave);
+                list.raise(WAVES == 1 ? all : below(all));
+            }
             const uint64_t lanes = __ballot(most > list.bar);
             if (lanes) {
                 if (!first && (uint32_t)__popcll(lanes) >= a.top) list.raise(bar_of(most, a.top));

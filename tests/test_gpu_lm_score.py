@@ -160,6 +160,18 @@ def test_orders_that_meet_the_selection_worst(ctx, dtype, classes, order):
         run(ctx, x, given, top=top)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,classes", [(3, 8192), (3, 9000), (500, 20000), (1, 1 << 20)])
+@pytest.mark.parametrize("few", [512, 1024, 2048, 3000])
+def test_equal_classes_where_few_come_first(ctx, dtype, rows, classes, few):
+    """The first classes hold a few better ones and no equals; all the others are equal, so the lowest numbers among them are the answer."""
+    x = torch.full((rows, classes), 5.0, dtype=DT[dtype], device="cuda")
+    x[:, :few] = 4.0
+    for top in (2, 10, 32):
+        x[:, : 16 * ((top + 3) // 4) : 16] = 6.0
+        run(ctx, x, np.array([[0, few - 1, few, classes - 1]] * rows), top=top)
+
+
 @pytest.mark.parametrize("rows", [1, 2, 7, 40, 300, 1500])
 def test_numbers_of_rows(ctx, rows):
     """From rows that many workgroups share to rows by the thousand; outputs and scratch used again by other calls."""
