@@ -365,7 +365,7 @@ mt_status mt_get_stats(const mt_ctx* ctx, mt_stats* out);
  * gain_ids[i] names row i's gain among n_gains (a tenant's); a row whose id is out of range gets y and y8 of zeros
  * (scales 1) and touches no gain.  gain_ids NULL: every row takes the first; gain NULL: no gain is applied.
  * Errors: MT_EINVAL (null, zero width, a stride below the width, eps negative or not finite, n_gains 0 with a gain),
- * MT_EUNSUPPORTED (dtype other than MT_F32 and MT_BF16), MT_ESTATE (host-only context), MT_EDEVICE. */
+ * MT_EUNSUPPORTED (dtype other than MT_F32 and MT_BF16, width over 2^24), MT_ESTATE (host-only context), MT_EDEVICE. */
 typedef struct {
     const void* x;              /* [rows][x_stride], dtype                     */
     const void* residual;       /* [rows][residual_stride], dtype, or NULL     */
@@ -402,7 +402,8 @@ mt_status mt_unregister_matrix4(mt_ctx* ctx, uint32_t matrix);
  * Columns of y from a matrix's out_features on, and rows in no group, are left as they are.
  * Groups come in the order of their rows and share none; a group of 0 rows is skipped.
  * Errors: MT_EINVAL (null, strides below a matrix's sizes, rows outside 0..rows or out of order), MT_ENOTFOUND (a
- * matrix that is not registered), MT_EUNSUPPORTED (types, activation), MT_ESTATE (host-only context), MT_EDEVICE. */
+ * matrix that is not registered), MT_EUNSUPPORTED (types, activation, a group of outputs beyond 2^23 workgroups of 16 x 16 or
+ * more each), MT_ESTATE (host-only context), MT_EDEVICE.  After an error the groups' outputs may be written in part. */
 typedef struct { uint32_t matrix, first_row, n_rows; } mt_row_group;
 typedef struct {
     const void* x;              /* [rows][x_stride], x_dtype                           */

@@ -14,7 +14,7 @@ namespace {
 
 constexpr uint32_t kMaxFeatures = 1u << 24;
 constexpr uint32_t kMinScale4 = 27, kMaxScale4 = 227;       // 2^-100 .. 2^100: no weight and no product of ordinary values leaves fp32's normal range
-constexpr uint64_t kMaxGrid = 0x7fffffffu;
+constexpr uint64_t kMaxGrid = 0xffffffffu / 512;         // a grid holds fewer than 2^32 threads
 
 #define LM_TRY(c, expr)                                                                                                     \
     do {                                                                                                                    \
@@ -59,6 +59,7 @@ mt_status mt_add_norm(mt_ctx* c, void* hip_stream, const mt_norm_args* a)
     if (a->rows && (!a->x || (!a->sum && !a->y && !a->y8))) return ctx_fail(c, MT_EINVAL, "null rows, or no output");
     if (a->rows && (a->y8 == nullptr) != (a->y8_scales == nullptr)) return ctx_fail(c, MT_EINVAL, "8-bit rows and their scales come together");
     if (a->width == 0) return ctx_fail(c, MT_EINVAL, "zero width");
+    if (a->width > kMaxFeatures) return ctx_fail(c, MT_EUNSUPPORTED, "rows of %u elements", a->width);
     if (!(a->eps >= 0.0f) || !std::isfinite(a->eps)) return ctx_fail(c, MT_EINVAL, "eps is negative or not finite");
     if (a->gain && a->n_gains == 0) return ctx_fail(c, MT_EINVAL, "a gain, but n_gains is 0");
     if (a->gain_ids && !a->gain) return ctx_fail(c, MT_EINVAL, "gain_ids without a gain");

@@ -4,6 +4,10 @@
 
 namespace mt {
 
+// A grid holds fewer than 2^32 threads: rows, of 1024 threads at most, that one launch takes.
+constexpr uint32_t kRowsAtOnce = 1u << 21;
+template <typename V> void move_rows(V*& p, uint64_t elements) { if (p) p += elements; }
+
 // Loads and stores of 16 or 8 bytes at any element's address.
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 template <typename T> struct Any;

@@ -168,7 +168,7 @@ hipError_t go(const mt_norm_args& a, bool stream, hipStream_t s)
 }
 
 template <typename T>
-hipError_t choose(const mt_norm_args& a, hipStream_t s)
+hipError_t launch(const mt_norm_args& a, hipStream_t s)
 {
     const uint64_t outputs = (uint64_t)a.rows * a.width * ((a.sum ? sizeof(T) : 0) + (a.y ? sizeof(T) : 0) + (a.y8 ? 1 : 0));
     const bool stream = outputs > kStreamBytes;
@@ -179,11 +179,29 @@ hipError_t choose(const mt_norm_args& a, hipStream_t s)
     return go<T, true, 2, true>(a, stream, s);
 }
 
+template <typename T>
+hipError_t all_rows(mt_norm_args a, hipStream_t s)
+{
+    for (uint32_t left = a.rows;; left -= kRowsAtOnce) {
+        a.rows = std::min(left, kRowsAtOnce);
+        const hipError_t e = launch<T>(a, s);
+        if (e != hipSuccess || left <= kRowsAtOnce) return e;
+        const uint64_t n = kRowsAtOnce;
+        a.x = (const T*)a.x + n * a.x_stride;
+        if (a.residual) a.residual = (const T*)a.residual + n * a.residual_stride;
+        move_rows(a.gain_ids, n);
+        if (a.sum) a.sum = (T*)a.sum + n * a.sum_stride;
+        if (a.y) a.y = (T*)a.y + n * a.y_stride;
+        move_rows(a.y8, n * a.y8_stride);
+        move_rows(a.y8_scales, n * a.y8_scales_stride);
+    }
+}
+
 }  // namespace
 
 hipError_t launch_norm(const mt_norm_args& a, hipStream_t s)
 {
-    return a.dtype == MT_BF16 ? choose<__bf16>(a, s) : choose<float>(a, s);
+    return a.dtype == MT_BF16 ? all_rows<__bf16>(a, s) : all_rows<float>(a, s);
 }
 
 }  // namespace mt

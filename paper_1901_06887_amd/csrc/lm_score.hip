@@ -495,6 +495,27 @@ hipError_t choose(const ScoreArgs& s, hipStream_t st)
     return mask ? go<T, false, true>(s, st) : go<T, false, false>(s, st);
 }
 
+template <typename T>
+hipError_t all_rows(ScoreArgs s, hipStream_t st)
+{
+    mt_score_args& a = s.a;
+    for (uint32_t left = a.rows;; left -= kRowsAtOnce) {
+        a.rows = std::min(left, kRowsAtOnce);
+        const hipError_t e = choose<T>(s, st);
+        if (e != hipSuccess || left <= kRowsAtOnce) return e;
+        const uint64_t n = kRowsAtOnce;           // (so many rows are never shared: no scratch)
+        a.logits = (const T*)a.logits + n * a.row_stride;
+        move_rows(a.n_classes, n);
+        move_rows(a.allowed, n * a.allowed_stride);
+        move_rows(a.given, n * a.n_given);
+        move_rows(a.given_logprobs, n * a.n_given);
+        move_rows(a.given_ranks, n * a.n_given);
+        move_rows(a.entropy, n);
+        move_rows(a.top_ids, n * a.top);
+        move_rows(a.top_logprobs, n * a.top);
+    }
+}
+
 }  // namespace
 
 // A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.  Handing over costs
@@ -520,7 +541,7 @@ uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t, uint32_t
 
 hipError_t launch_score(const ScoreArgs& a, hipStream_t s)
 {
-    return a.a.dtype == MT_BF16 ? choose<__bf16>(a, s) : choose<float>(a, s);
+    return a.a.dtype == MT_BF16 ? all_rows<__bf16>(a, s) : all_rows<float>(a, s);
 }
 
 }  // namespace mt

@@ -179,6 +179,26 @@ def test_offsets_past_32_bits(ctx):
     check(x.double().cpu().numpy(), 1.0, 1e-6, "bf16", y.double().cpu().numpy())
 
 
+def test_more_rows_than_a_grid_of_threads(ctx):
+    rows, width = (2 << 21) + 3, 4
+    x, r = torch.randn(rows, width, device="cuda"), torch.randn(rows, width, device="cuda")
+    gain, ids = torch.randn(5, width, device="cuda"), torch.randint(-1, 6, (rows,), dtype=torch.int32, device="cuda")
+    s, y = torch.empty_like(x), torch.empty_like(x)
+    q, e = torch.empty(rows, width, dtype=torch.uint8, device="cuda"), torch.empty(rows, 1, dtype=torch.uint8, device="cuda")
+    mt.add_norm(ctx, x, residual=r, gain=gain, gain_ids=ids, sum_out=s, out=y, out8=q.view(torch.float8_e4m3fn), out8_scales=e)
+    h = x + r
+    assert torch.equal(s, h)
+    known = (ids >= 0) & (ids < 5)
+    g = gain.double()[ids.clamp(0, 4).long()] * known.double()[:, None]
+    want = h.double() * torch.rsqrt((h.double() ** 2).mean(1, keepdim=True) + 1e-6) * g
+    assert bool(((y.double() - want).abs() <= (REL + HALF_ULP["f32"]) * want.abs() + 1e-38).all())
+    for first in (0, (1 << 21) - 5, (2 << 21) - 5, rows - 8):                    # the 8-bit rows are those of calls of a few rows
+        few = slice(first, first + 8)
+        q1, e1 = torch.empty(8, width, dtype=torch.uint8, device="cuda"), torch.empty(8, 1, dtype=torch.uint8, device="cuda")
+        mt.add_norm(ctx, x[few], residual=r[few], gain=gain, gain_ids=ids[few], out8=q1.view(torch.float8_e4m3fn), out8_scales=e1)
+        assert torch.equal(q[few], q1) and torch.equal(e[few], e1)
+
+
 def test_on_another_stream_and_in_a_graph(ctx):
     x = torch.randn(40, 4096, dtype=torch.bfloat16, device="cuda")
     want, y = torch.empty_like(x), torch.empty_like(x)

@@ -233,6 +233,25 @@ def test_offsets_past_32_bits(ctx):
     run(ctx, x, np.array([[1], [2], [4999]]), top=4)
 
 
+def test_more_rows_than_a_grid_of_threads(ctx):
+    rows, classes = (2 << 21) + 3, 40
+    x = torch.randn(rows, classes, device="cuda").to(torch.bfloat16)
+    given = torch.randint(0, classes, (rows, 2), dtype=torch.int32, device="cuda")
+    n = torch.randint(0, classes + 1, (rows,), dtype=torch.int32, device="cuda")
+    allowed = torch.randint(-(1 << 31), 1 << 31, (rows, 2), dtype=torch.int64, device="cuda").to(torch.int32)
+    o = mt.alloc_scores(rows, 2, 3)
+    mt.score(ctx, x, o, given=given, n_classes=n, allowed=allowed)
+    torch.cuda.synchronize()
+    for first in (0, (1 << 21) - 5, (2 << 21) - 5, rows - 8):
+        few = slice(first, first + 8)
+        ref = lm.scored(x[few].double().cpu().numpy(), n[few].cpu().numpy(), allowed[few].cpu().numpy().view(np.uint32), given[few].cpu().numpy(), 3)
+        agree(mt.Scores(o.given_logprobs[few], o.given_ranks[few], o.entropy[few], o.top_ids[few], o.top_logprobs[few], o.scratch), ref, 2, 3)
+    c = torch.arange(classes, device="cuda")
+    ok = (c < n[:, None]) & ((allowed[:, c // 32] >> (c % 32)) & 1).bool()
+    assert bool(((o.top_ids >= 0).sum(1) == ok.sum(1).clamp(max=3)).all())
+    assert torch.equal(o.top_ids[:, 0].long(), torch.where(ok.any(1), torch.where(ok, x.double(), -1e300).argmax(1), -1))
+
+
 def test_streams_and_graphs(ctx):
     rng = np.random.default_rng(3)
     xs = [logits(rng, 2, 60000, "bf16") for _ in range(4)]

@@ -113,6 +113,8 @@ def test_add_norm_refuses():
                        (dict(gain_ids=64), 1), (dict(y8=64, y8_stride=100), 1), (dict(y8_scales=64, y8_scales_stride=4), 1), (dict(y8=64, y8_stride=100, y8_scales=64, y8_scales_stride=3), 1),
                        (dict(sum=64, sum_stride=1), 1), (dict(eps=-1e-6), 1), (dict(eps=float("inf")), 1), ({}, 7)):
         refused(status, c.add_norm, 0, norm_args(**kw))
+    wide = (1 << 24) + 1
+    refused(5, c.add_norm, 0, norm_args(width=wide, x_stride=wide, y_stride=wide))
     assert B.load_library().mt_add_norm(c._h, None, None) == 1 and B.load_library().mt_add_norm(None, None, ctypes.byref(norm_args())) == 1
     c.close()
 
