@@ -426,6 +426,9 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
             }
         }
     };
+    f32x4 bias[kNt * RT / kQuarters];
+#pragma unroll
+    for (int i = 0; i < kNt * RT / kQuarters; ++i) bias[i] = bias_of(a, g, (slab * kNt + (i * kQuarters + quarter) / RT) * kTile4Rows + 4 * lq);
     // Whole k tiles, in rounds of four.  A quarter whose turn finds none left asks for the last one again and multiplies nothing: with loads inside
     // of conditions the compiler's counts of what is in flight would make every round wait for all of it.
     u32x4* tiles = lds + quarter * 2 * kTileVecs;
@@ -462,9 +465,6 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
         if (mine) multiply(wl, tiles);
     }
     // quarter q finishes the tiles t with t % 4 = q of its slab, with the sums of the other quarters
-    f32x4 bias[kNt * RT / kQuarters];
-#pragma unroll
-    for (int i = 0; i < kNt * RT / kQuarters; ++i) bias[i] = bias_of(a, g, (slab * kNt + (i * kQuarters + quarter) / RT) * kTile4Rows + 4 * lq);
     __syncthreads();
     f32x4* part = (f32x4*)lds;
     const auto at = [&](uint32_t q, uint32_t t) { return ((q * kSlabs + wave % kSlabs) * (kNt * RT) + t) * 64 + lane; };
