@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
     __shared__ f32x4 part[kWaves4][NT][64];
 #pragma unroll
     for (int n = 0; n < NT; ++n) if (n != (int)wave) part[wave][n][lane] = acc[n];
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         if (n != (int)wave) continue;
@@ -465,12 +465,12 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
         if (mine) multiply(wl, tiles);
     }
     // quarter q finishes the tiles t with t % 4 = q of its slab, with the sums of the other quarters
-    __syncthreads();
+    lds_barrier();
     f32x4* part = (f32x4*)lds;
     const auto at = [&](uint32_t q, uint32_t t) { return ((q * kSlabs + wave % kSlabs) * (kNt * RT) + t) * 64 + lane; };
 #pragma unroll
     for (int t = 0; t < kNt * RT; ++t) if (t % kQuarters != (int)quarter) part[at(quarter, t)] = acc[t / RT][t % RT];
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int t = 0; t < kNt * RT; ++t) {
         if (t % kQuarters != (int)quarter) continue;
