@@ -94,7 +94,7 @@ mt_status mt_register_matrix4(mt_ctx* c, uint32_t N, uint32_t K, const uint8_t* 
             return ctx_fail(c, MT_EUNSUPPORTED, "scale %u of output %zu is outside %u..%u", scales[i], i / div_up(K, MT_MX_BLOCK), kMinScale4, kMaxScale4);
     const CtxView v = ctx_view(c);
     Matrix4 m;
-    m.used = true; m.has_bias = bias != nullptr; m.N = N; m.K = K; m.len = matrix4_bytes(N, K);
+    m.used = true; m.N = N; m.K = K; m.len = matrix4_bytes(N, K);
     try {
         size_t at = 0;
         while (at < v.matrices->size() && (*v.matrices)[at].used) ++at;
@@ -181,7 +181,7 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
             LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
             k.n_groups = 0; grid = 0;
         }
-        k.groups[k.n_groups++] = Group4{m.off, m.N, m.K, r.first_row, r.n_rows, (uint32_t)grid, m.has_bias ? 1u : 0u};
+        k.groups[k.n_groups++] = Group4{m.off, m.N, m.K, r.first_row, r.n_rows, (uint32_t)grid};
         grid += wgs;
     }
     LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));

@@ -199,16 +199,13 @@ __device__ __forceinline__ void store_outputs(const Linear4Args& a, uint64_t row
         for (uint32_t i = 0; i < 4; ++i) if (n0 + i < N) y[i] = (Y)v[i];
 }
 
-// The biases of four outputs; zeros where there are none.
+// The biases of four outputs, in loads that no branch holds up; past the last output, its own.
 __device__ __forceinline__ f32x4 bias_of(const Linear4Args& a, const Group4& g, uint32_t n0)
 {
-    f32x4 b = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (!g.has_bias) return b;
     const float* p = (const float*)(a.arena + g.off + matrix4_tiles_bytes(g.N, g.K));
-    if (n0 + 4 <= g.N) b = __builtin_bit_cast(f32x4, *(const Any<float>::vec16*)(p + n0));
-    else
+    f32x4 b;
 #pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) if (n0 + i < g.N) b[i] = p[n0 + i];
+    for (uint32_t i = 0; i < 4; ++i) b[i] = p[min(n0 + i, g.N - 1)];
     return b;
 }
 
@@ -224,12 +221,19 @@ __device__ __forceinline__ void finish_tile(const Linear4Args& a, const Group4& 
     else store_outputs<float>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
 }
 
-// A workgroup's group: the last one that starts at or before it.
-__device__ __forceinline__ uint32_t group_of(const Linear4Args& a, uint32_t lane)
+// A workgroup's group: the last one that starts at or before it.  (What a kernel reads of its arguments is asked for in one go and waited for here: loads
+// where they are used are as many trips to memory one after the other, some 500 clocks each in a launch's first workgroups.)
+__device__ __forceinline__ Group4 group_of(const Linear4Args& a, uint32_t lane)
 {
-    if (a.n_groups == 1) return 0;
-    const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
-    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1);
+    Group4 g = a.groups[0];
+    asm volatile("" :: "s"(a.arena), "s"(a.x), "s"(a.x_scales), "s"(a.y), "s"(a.x_stride), "s"(a.x_scales_stride), "s"(a.y_stride), "s"(a.act), "s"(a.n_groups), "s"(a.y_bf16),
+                 "s"(g.off), "s"(g.N), "s"(g.K), "s"(g.row0), "s"(g.n_rows));
+    if (a.n_groups > 1) {
+        const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
+        g = a.groups[__builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1)];
+        asm volatile("" :: "s"(g.off), "s"(g.N), "s"(g.K), "s"(g.row0), "s"(g.n_rows), "s"(g.wg_base));
+    }
+    return g;
 }
 
 constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles and add their sums up through LDS
@@ -239,7 +243,7 @@ template <Kind KIND, int NT, int DEPTH>
 __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Group4& g = a.groups[group_of(a, lane)];
+    const Group4 g = group_of(a, lane);
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_slabs = ceil_div(n_tiles, NT);
     const uint32_t local = blockIdx.x - g.wg_base;
@@ -384,7 +388,7 @@ __global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
     constexpr uint32_t kParts = KIND == kRowsF32 ? 3 : 1, kPartVecs = 16 * RT * 16, kTileVecs = kParts * kPartVecs;      // a k tile of the rows, in 16 bytes
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t quarter = wave / kSlabs, li = lane & 15, lq = lane >> 4;
-    const Group4& g = a.groups[group_of(a, lane)];
+    const Group4 g = group_of(a, lane);
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_wide = ceil_div(n_tiles, kNt * kSlabs), chunks = ceil_div(g.n_rows, 16 * RT);
     // workgroups eight apart share an XCD: they take the same outputs of one chunk of rows after the other

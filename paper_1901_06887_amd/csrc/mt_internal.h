@@ -314,12 +314,12 @@ hipError_t launch_image_ops(const GapArgs& a, uint32_t slices, hipStream_t s);  
 hipError_t launch_head(const HeadArgs& a, hipStream_t s);
 
 // ---- operators of language models' answers (lm_api.cpp, lm_*.hip) ---------------------------
-// A 4-bit matrix as it lies in the arena: tiles of 16 outputs x 128 of the fan-in, [output tile][k tile], then the fp32 biases (if any).
+// A 4-bit matrix as it lies in the arena: tiles of 16 outputs x 128 of the fan-in, [output tile][k tile], then the fp32 biases, zeros where there are none.
 // A tile is one operand of the matrix instructions: lane l holds output l % 16 and the 32 values of k block l / 16, 16 bytes of
 // codes in lane order, then 64 bytes of scales in lane order; outputs and k past the matrix are zero with scale 1.
 constexpr uint32_t kTile4Rows = 16, kTile4K = 128, kTile4Codes = 1024, kTile4Bytes = kTile4Codes + 64;
 struct Matrix4 {
-    bool used = false, has_bias = false;
+    bool used = false;
     uint32_t N = 0, K = 0;
     uint64_t off = 0, len = 0;       // the arena block
 };
@@ -332,7 +332,6 @@ struct Group4 {
     uint64_t off;                    // arena offset of the matrix
     uint32_t N, K, row0, n_rows;
     uint32_t wg_base;                // workgroups of the launch's groups before this one
-    uint32_t has_bias;
 };
 struct Linear4Args {
     const uint8_t* arena;
