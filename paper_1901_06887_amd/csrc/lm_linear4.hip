@@ -177,13 +177,18 @@ template <Kind KIND, int NT> struct Step {
     }
 };
 
-// NaN stays NaN in both.  GELU: the library's erfc where fp32 is written; for bf16 the formula of the fully-connected layers (some 1e-7 off, a quarter of
-// the instructions), kept from multiplying an infinity by 0.
-__device__ __forceinline__ float activate4(float z, uint32_t act, uint32_t to_bf16)
+// NaN stays NaN in all.
+__device__ __forceinline__ float relu4(float z) { return z < 0.0f ? 0.0f : z; }
+__device__ __forceinline__ float gelu4(float z) { return 0.5f * z * erfcf(-0.70710678f * z); }
+// For bf16, some 3e-7 off at a quarter of the instructions: max(z, 0) - a q with a = |z| and q = normal tail beyond a = t P(t) exp(-a^2 / 2), t = 1 / (1 + p a)
+// (Abramowitz and Stegun 7.1.26).  From 64 on q is 0 in fp32; a stays below so that no infinity meets it.
+__device__ __forceinline__ float gelu4_bf16(float z)
 {
-    if (act == MT_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (!to_bf16) return 0.5f * z * erfcf(-0.70710678f * z);
-    return fabsf(z) < 64.0f ? gelu(z) : z > 0.0f ? z : z < 0.0f ? -0.0f : z;
+    const float a = fminf(fabsf(z), 64.0f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.231641888f, a, 1.0f));       // (0.3275911 / sqrt(2))
+    const float poly = t * (0.127414796f + t * (-0.142248368f + t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f))));
+    const float e = __builtin_amdgcn_exp2f(-0.72134752f * a * a);             // (log2(e) / 2)
+    return fmaf(-a, poly * e, relu4(z));
 }
 
 __device__ __forceinline__ void store4(__bf16* p, const f32x4& v) { *(Any<__bf16>::vec8*)p = Any<__bf16>::vec8{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
@@ -213,10 +218,10 @@ __device__ __forceinline__ f32x4 bias_of(const Linear4Args& a, const Group4& g, 
 __device__ __forceinline__ void finish_tile(const Linear4Args& a, const Group4& g, uint32_t n0, uint32_t in_group, f32x4 v)
 {
     if (in_group >= g.n_rows || n0 >= g.N) return;
-    if (a.act != MT_ACT_NONE) {
-#pragma unroll
-        for (uint32_t i = 0; i < 4; ++i) v[i] = activate4(v[i], a.act, a.y_bf16);
-    }
+    if (a.act == MT_ACT_GELU) {
+        if (a.y_bf16) v = f32x4{gelu4_bf16(v[0]), gelu4_bf16(v[1]), gelu4_bf16(v[2]), gelu4_bf16(v[3])};
+        else v = f32x4{gelu4(v[0]), gelu4(v[1]), gelu4(v[2]), gelu4(v[3])};
+    } else if (a.act == MT_ACT_RELU) v = f32x4{relu4(v[0]), relu4(v[1]), relu4(v[2]), relu4(v[3])};
     if (a.y_bf16) store_outputs<__bf16>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
     else store_outputs<float>(a, (uint64_t)g.row0 + in_group, n0, g.N, v);
 }
