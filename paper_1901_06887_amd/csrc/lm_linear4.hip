@@ -111,27 +111,22 @@ template <Kind KIND> struct RawRow {
     }
 };
 
-// ... and as operands of four 16x16x32 instructions (times three for fp32).
+// ... the j-th eight of them as an operand of a 16x16x32 instruction (of three for fp32).
 template <Kind KIND> struct RowOperand {
     static constexpr int kParts = KIND == kRowsF32 ? 3 : 1;
-    u32x4 v[kParts][4];
-    __device__ __forceinline__ explicit RowOperand(const RawRow<KIND>& r)
+    u32x4 v[kParts];
+    __device__ __forceinline__ RowOperand(const RawRow<KIND>& r, int j)
     {
+        if constexpr (KIND == kRowsBf16) v[0] = r.v[j];
+        else if constexpr (KIND == kRowsMx8) v[0] = eight_of(r.v[j / 2][2 * (j % 2)], r.v[j / 2][2 * (j % 2) + 1], scale_of(r.scale));
+        else
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (KIND == kRowsBf16) v[0][j] = r.v[j];
-            else if constexpr (KIND == kRowsF32) {
+            for (int h = 0; h < 2; ++h) {
+                uint32_t part[3][2];
+                split3(r.v[2 * j + h], part);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t part[3][2];
-                    split3(r.v[2 * j + h], part);
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) { v[q][j][2 * h] = part[q][0]; v[q][j][2 * h + 1] = part[q][1]; }
-                }
-            } else if constexpr (KIND == kRowsMx8) {
-                v[0][j] = eight_of(r.v[j / 2][2 * (j % 2)], r.v[j / 2][2 * (j % 2) + 1], scale_of(r.scale));
+                for (int q = 0; q < 3; ++q) { v[q][2 * h] = part[q][0]; v[q][2 * h + 1] = part[q][1]; }
             }
-        }
     }
 };
 
@@ -162,18 +157,17 @@ template <Kind KIND, int NT> struct Step {
 
     __device__ __forceinline__ void multiply(f32x4 (&acc)[NT]) const
     {
-        const RowOperand<KIND> o(x);
-        u32x4 wv[NT][4];
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int j = 0; j < 4; ++j) {
+            const RowOperand<KIND> o(x, j);
+            u32x4 wv[NT];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) wv[n][j] = weights_of(w[n], j);
+            for (int n = 0; n < NT; ++n) wv[n] = weights_of(w[n], j);
 #pragma unroll
-        for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
+            for (int p = RowOperand<KIND>::kParts - 1; p >= 0; --p)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) acc[n] = mfma(wv[n][j], o.v[p][j], acc[n]);
+                for (int n = 0; n < NT; ++n) acc[n] = mfma(wv[n], o.v[p], acc[n]);
+        }
     }
 };
 
@@ -245,7 +239,7 @@ constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles 
 
 // A workgroup serves 16 NT outputs of 16 rows of a group; a wave asks for DEPTH k tiles at a time, the next ones before it multiplies.
 template <Kind KIND, int NT, int DEPTH>
-__global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
+__global__ void __launch_bounds__(kWaves4 * 64, KIND == kRowsF32 ? 3 : 2) linear4_kernel(Linear4Args a)
 {
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Group4 g = group_of(a, lane);
@@ -263,6 +257,8 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
     f32x4 acc[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) acc[n] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const f32x4 bias = bias_of(a, g, (slab * NT + wave) * kTile4Rows + 4 * lq);       // for the tile that this wave finishes
 
     // whole k tiles: this wave's are wave, wave + 4, ...
     const uint32_t whole = K / kTile4K;
@@ -305,7 +301,6 @@ __global__ void __launch_bounds__(kWaves4 * 64) linear4_kernel(Linear4Args a)
 
     // tile n is finished by wave n
     static_assert(NT <= kWaves4, "a wave finishes one tile at most");
-    const f32x4 bias = bias_of(a, g, (slab * NT + wave) * kTile4Rows + 4 * lq);
     __shared__ f32x4 part[kWaves4][NT][64];
 #pragma unroll
     for (int n = 0; n < NT; ++n) if (n != (int)wave) part[wave][n][lane] = acc[n];
