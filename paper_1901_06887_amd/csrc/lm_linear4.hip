@@ -520,12 +520,14 @@ hipError_t prepare_rows() { return hipFuncSetAttribute((const void*)linear4_rows
 }  // namespace
 
 // Kernel times (us) of the three forms, 16 x 16 tiles with a workgroup for 16 outputs / for 64 / rows through LDS:
-//   bf16, 24 rows through 4864 x 832 8.5 / 8.7 / 12.8, three tenants of them 14.2 / 9.6 / 13.6; 64 rows through 4096 x 4096 18.6 / 8.7 / 18.5, two tenants
-//   35.6 / 13.7 / 19.0, four 67.5 / 24.4 / 20.6; 40 tenants of 64 rows through 448 x 960 85 / 19.6 / 20.5; one row through 4096 x 8192 6.1 / 7.2, x 32768 16.5 / 13.1
-//   fp32, 64 rows through 4096 x 4096 40.9 / 18.1 / 19.9, two tenants 76.2 / 34.6 / 21.8; 8 tenants of 64 rows through 1024 x 1024 24.2 / 15.1 / 9.6; one row
-//   through 4096 x 32768 64.6 / 31.0 / 21.7
+//   bf16, 24 rows through 4864 x 832 8.4 / 8.7 / 13.0, three tenants of them 14.3 / 9.7 / 13.7; 16 rows through 4096 x 4096 7.2 / 8.2 / 11.9, 24 rows 9.8 / 8.3 / 11.9,
+//   64 18.6 / 8.7 / 18.5, two tenants of those 34.9 / 14.2 / 18.8, four 66.9 / 24.6 / 20.6; 40 tenants of 64 rows through 448 x 960 84 / 17.0 / 20.2; one row through
+//   4096 x 8192 6.2 / 6.7, x 32768 16.7 / 12.8
+//   fp32, 64 rows through 4096 x 4096 40.9 / 18.2 / 18.6, two tenants 76.3 / 30.3 / 20.7; 8 tenants of 64 rows through 1024 x 1024 24.3 / 11.8 / 9.4; one row
+//   through 4096 x 4096 12.0 / 14.3, x 8192 19.1 / 14.8, x 32768 63.2 / 26.5 / 20.4
 // So rows go through LDS where that makes half as many workgroups as there are compute units (fp32, whose every value is split: three quarters, and for few
-// rows too) of two k tiles or more to a wave; else a workgroup takes 64 outputs where that makes one for every compute unit, or for every fourth where several rows are read.
+// rows too) of two k tiles or more to a wave; else a workgroup takes 64 outputs where workgroups for 16 would be more than the compute units, or four times as many
+// where few rows are read and not split.
 Linear4Shape linear4_shape(uint64_t row_tiles, uint32_t most_rows, uint32_t most_k, uint32_t n_cus, uint32_t x_dtype)
 {
     const bool f32 = x_dtype == MT_F32;
@@ -535,7 +537,7 @@ Linear4Shape linear4_shape(uint64_t row_tiles, uint32_t most_rows, uint32_t most
     s.through_lds = (f32 || most_rows > 16) && row_tiles / (s.nt * s.rt) >= (f32 ? 3 * n_cus / 4 : n_cus / 2) && most_k >= 2 * kQuarters * kTile4K;
     if (!s.through_lds) {
         s.rt = 1;
-        s.nt = row_tiles / 4 >= (most_rows > 4 ? n_cus / 4 : n_cus) ? 4 : 1;
+        s.nt = row_tiles > (most_rows > 4 || f32 ? n_cus : 4 * n_cus - 1) ? 4 : 1;
     }
     return s;
 }
