@@ -42,6 +42,28 @@ __device__ __forceinline__ void split3(const u32x4& x, uint32_t (&part)[3][2])
     }
 }
 
+// The same at half the instructions where the wave has neither an infinity nor a NaN.  (Where the waves wait for this, through LDS: four tenants of 64 rows through
+// 4096 x 4096 40.1 -> 35.1 us.  Where they wait for loads the branch costs more: one row 12.0 -> 12.5.)
+__device__ __forceinline__ void split3_mostly_finite(const u32x4& x, uint32_t (&part)[3][2])
+{
+    const f32x4 f = __builtin_bit_cast(f32x4, x);
+    const float zero = fmaf(f[3], 0.0f, fmaf(f[2], 0.0f, fmaf(f[1], 0.0f, f[0] * 0.0f)));
+    if (__ballot(zero != 0.0f)) { split3(x, part); return; }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        uint32_t p[3][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            p[0][h] = __builtin_bit_cast(uint32_t, f[2 * i + h]);
+            const float r = f[2 * i + h] - __builtin_bit_cast(float, p[0][h] & 0xffff0000u);
+            p[1][h] = __builtin_bit_cast(uint32_t, r);
+            p[2][h] = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, p[1][h] & 0xffff0000u));
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q) part[q][i] = __builtin_amdgcn_perm(p[q][1], p[q][0], 0x07060302);       // the upper halves
+    }
+}
+
 // 2^(byte - 127); the smallest is subnormal, the largest byte is NaN.
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __builtin_bit_cast(float, byte == 0xff ? 0x7fc00000u : byte ? byte << 23 : 0x00400000u); }
 // Eight 8-bit values, scaled, as bf16.
@@ -369,7 +391,7 @@ template <Kind KIND, int RT> struct RowFetch {
             if constexpr (KIND == kRowsBf16) to[place(row, u)] = v[i];
             else if constexpr (KIND == kRowsF32) {
                 uint32_t part[3][2];
-                split3(v[i], part);
+                split3_mostly_finite(v[i], part);
 #pragma unroll
                 for (uint32_t q = 0; q < 3; ++q) *((u32x2*)(to + q * (16 * RT * 16) + place(row, u / 2)) + u % 2) = u32x2{part[q][0], part[q][1]};
             } else {
@@ -523,8 +545,8 @@ hipError_t prepare_rows() { return hipFuncSetAttribute((const void*)linear4_rows
 //   bf16, 24 rows through 4864 x 832 8.4 / 8.7 / 13.0, three tenants of them 14.3 / 9.7 / 13.7; 16 rows through 4096 x 4096 7.2 / 8.2 / 11.9, 24 rows 9.8 / 8.3 / 11.9,
 //   64 18.6 / 8.7 / 18.5, two tenants of those 34.9 / 14.2 / 18.8, four 66.9 / 24.6 / 20.6; 40 tenants of 64 rows through 448 x 960 84 / 17.0 / 20.2; one row through
 //   4096 x 8192 6.2 / 6.7, x 32768 16.7 / 12.8
-//   fp32, 64 rows through 4096 x 4096 40.9 / 18.2 / 18.6, two tenants 76.3 / 30.3 / 20.7; 8 tenants of 64 rows through 1024 x 1024 24.3 / 11.8 / 9.4; one row
-//   through 4096 x 4096 12.0 / 14.3, x 8192 19.1 / 14.8, x 32768 63.2 / 26.5 / 20.4
+//   fp32, 64 rows through 4096 x 4096 40.9 / 18.2 / 18.6, two tenants 76.3 / 30.3 / 18.4; 8 tenants of 64 rows through 1024 x 1024 24.3 / 11.8 / 9.2; one row
+//   through 4096 x 4096 12.0 / 14.3, x 8192 19.1 / 14.8, x 32768 63.2 / 26.5 / 19.9
 // So rows go through LDS where that makes half as many workgroups as there are compute units (fp32, whose every value is split: three quarters, and for few
 // rows too) of two k tiles or more to a wave; else a workgroup takes 64 outputs where workgroups for 16 would be more than the compute units, or four times as many
 // where few rows are read and not split.
