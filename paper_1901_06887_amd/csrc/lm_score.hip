@@ -476,9 +476,12 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
 template <typename T, bool TOP, bool MASK>
 hipError_t go(const ScoreArgs& s, hipStream_t st)
 {
-    // A wave to a row where rows are short, or many for their length (us, four waves / one, 5 alternatives, fp32 and bf16: 256 rows of 4000 classes 8.2 / 11.7 and
-    // 9.8 / 10.3, 1024 rows 12.8 / 13.5 and 14.1 / 11.5; 2048 rows of 4000 19.9 / 15.7 and 24.5 / 13.8, of 8192 27.0 / 23.1 and 24.8 / 18.6, of 32768 67 / 75 and 54 / 53).
-    if (s.parts == 1 && (s.a.classes <= 2 * kSome || (s.a.classes <= 8 * kSome && s.a.classes <= 4 * (uint64_t)s.a.rows)))
+    // A wave to a row where rows are short, or many for their length (us, four waves / one, 5 alternatives, fp32 and bf16: 256 rows of 1000 classes 7.9 / 6.4 and
+    // 9.7 / 8.1, of 4000 7.8 / 11.1 and 9.6 / 10.3; 600 rows of 3000 9.8 / 10.0 and 11.2 / 10.0, of 8192 13.4 / 17.2 and 10.8 / 14.0; 1024 rows of 4000 11.4 / 13.0 and
+    // 13.4 / 11.1, of 10000 18.0 / 22.1 and 17.4 / 16.9, of 16384 21.1 / 28.3 and 18.5 / 21.9; 2048 rows of 4000 17.8 / 15.0 and 22.1 / 12.5, of 12000 31.5 / 31.4 and
+    // 30.9 / 23.2, of 24576 47.8 / 52.0 and 38.2 / 35.8).  fp32, two bytes more a class to wait for, needs two waves to every SIMD.
+    const bool many = sizeof(T) == 4 ? s.a.rows >= 2048 && s.a.classes <= 12 * kSome : s.a.classes <= 24 * kSome && s.a.classes <= 10 * (uint64_t)s.a.rows;
+    if (s.parts == 1 && (s.a.classes <= 2 * kSome || many))
         hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(64 * kWaves), 0, st, s);
     else if (s.parts == 1)
         hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false>), dim3(s.a.rows), dim3(64 * kWaves), 0, st, s);
@@ -518,18 +521,18 @@ hipError_t all_rows(ScoreArgs s, hipStream_t st)
 
 }  // namespace
 
-// A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.  Handing over costs
-// some 4 us, a chunk more for every wave 1.7: two parts do not pay (64 rows of 8192 classes, 5 alternatives: 9.9 us whole, 11.2 in two parts; one row of
-// 10000 10.7 whole, 12.3 in two, 10.2 in three; 16 rows of 65001 60.6 whole, 34.9 in four, 17.4 in 16; 256 rows of 32768 23.9 whole, 20.9 in four).
+// A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.  Handing over costs some 4 us,
+// and few parts save little (us whole / in parts, 5 alternatives, fp32 and bf16: one row of 16384 10.2 / 10.4 and 9.4 / 10.4, of 24576 12.8 / 10.8 and 10.4 / 10.9, of 65536
+// 22.9 / 10.9 and 18.7 / 10.8; 128 rows of 16384 12.6 / 12.8 and 11.2 / 12.8, of 24576 16.0 / 14.8 and 13.3 / 14.2, of 65536 31.7 / 23.5 and 22.8 / 18.7; 256 rows, in four,
+// of 32768 20.6 / 20.3 and 16.0 / 19.4, of 65536 35.4 / 29.8 and 23.3 / 24.3, of 131072 65.8 / 43.4 and 39.6 / 33.8).
 void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len)
 {
     *parts = 1; *part_len = classes;
     if (rows == 0) return;
     const uint32_t span = kSome * kWaves, spans = (classes + span - 1) / span, want = std::min(kMaxParts, kRecords / rows);
-    if (spans < 3 || want < 3) return;
+    if (want < 3 || spans < (want < 8 ? 16u : 5u)) return;
     *part_len = (spans + want - 1) / want * span;
     *parts = (uint32_t)(((uint64_t)classes + *part_len - 1) / *part_len);
-    if (*parts < 3) *parts = 1, *part_len = classes;
 }
 
 uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t, uint32_t)
