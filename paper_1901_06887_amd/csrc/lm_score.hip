@@ -161,7 +161,7 @@ __device__ __forceinline__ float bar_of(float v, uint32_t n)
     return __builtin_bit_cast(float, lo & 0x80000000u ? lo ^ 0x80000000u : ~lo);
 }
 
-// A lane's 16 classes of a chunk as they come from memory: vectors of 16 bytes, 64 of them side by side.
+// A lane's classes of a chunk as they come from memory: vectors of 16 bytes, 64 of them side by side.
 template <typename T, uint32_t VECS> struct Raw {
     static constexpr uint32_t kVec = 16 / sizeof(T), kVecs = VECS, kPer = kVec * kVecs, kChunk = 64 * kPer;      // ... a lane's and a wave's classes at a time
     u32x4 v[kVecs];
@@ -252,12 +252,11 @@ struct Share {
     uint32_t in_front;        // lane g: allowed classes in front of given class g
 };
 
-// WAVES waves share a row's part [blockIdx.y]; WAVES 1: every wave of the workgroup has a row of its own.
-template <typename T, bool TOP, bool MASK, uint32_t WAVES, bool PARTS>
+// WAVES waves share a row's part [blockIdx.y]; WAVES 1: every wave of the workgroup has a row of its own.  A lane takes VECS vectors of 16 bytes at a time.
+template <typename T, bool TOP, bool MASK, uint32_t WAVES, bool PARTS, uint32_t VECS>
 __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
 {
-    // (four vectors keep the memory busy: 2048 rows of 32768 bf16 classes 54 -> 50 us; where the row is shared they would leave waves without classes)
-    using R = Raw<T, PARTS && sizeof(T) == 2 ? 2 : 4>;
+    using R = Raw<T, VECS>;
     constexpr uint32_t kPer = R::kPer, kChunk = R::kChunk;
     const mt_score_args& a = s.a;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -476,17 +475,23 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
 template <typename T, bool TOP, bool MASK>
 hipError_t go(const ScoreArgs& s, hipStream_t st)
 {
-    // A wave to a row where rows are short, or many for their length (us, four waves / one, 5 alternatives, fp32 and bf16: 256 rows of 1000 classes 7.9 / 6.4 and
-    // 9.7 / 8.1, of 4000 7.8 / 11.1 and 9.6 / 10.3; 600 rows of 3000 9.8 / 10.0 and 11.2 / 10.0, of 8192 13.4 / 17.2 and 10.8 / 14.0; 1024 rows of 4000 11.4 / 13.0 and
-    // 13.4 / 11.1, of 10000 18.0 / 22.1 and 17.4 / 16.9, of 16384 21.1 / 28.3 and 18.5 / 21.9; 2048 rows of 4000 17.8 / 15.0 and 22.1 / 12.5, of 12000 31.5 / 31.4 and
-    // 30.9 / 23.2, of 24576 47.8 / 52.0 and 38.2 / 35.8).  fp32, two bytes more a class to wait for, needs two waves to every SIMD.
-    const bool many = sizeof(T) == 4 ? s.a.rows >= 2048 && s.a.classes <= 12 * kSome : s.a.classes <= 24 * kSome && s.a.classes <= 10 * (uint64_t)s.a.rows;
-    if (s.parts == 1 && (s.a.classes <= 2 * kSome || many))
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false>), dim3((s.a.rows + kWaves - 1) / kWaves), dim3(64 * kWaves), 0, st, s);
-    else if (s.parts == 1)
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false>), dim3(s.a.rows), dim3(64 * kWaves), 0, st, s);
-    else
-        hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, true>), dim3(s.a.rows, s.parts), dim3(64 * kWaves), 0, st, s);
+    // A wave to a row where rows are short, or many for their length (us, four waves / one, 5 alternatives, fp32 and bf16: 256 rows of 1000 classes 7.9 / 6.3 and
+    // 7.9 / 6.3, of 4000 7.8 / 11.1 and 7.5 / 9.7; 1024 rows of 2000 10.3 / 8.8 and 9.9 / 8.0, of 4000 11.4 / 13.0 and 10.7 / 11.0, of 8192 15.6 / 17.9 and 13.9 / 14.7, of
+    // 10000 18.0 / 22.1 and 17.4 / 16.9, of 16384 21.1 / 28.3 and 18.5 / 21.9; 2048 rows of 4000 17.8 / 15.0 and 17.0 / 13.2, of 12000 31.5 / 31.4 and 30.9 / 23.2, of 24576
+    // 47.8 / 52.0 and 38.2 / 35.8).  fp32, with more bytes to wait for, needs two waves to every SIMD.
+    const bool many = sizeof(T) == 4 ? s.a.rows >= 2048 && s.a.classes <= 12 * kSome
+                                     : s.a.classes <= 24 * kSome && s.a.classes <= (s.a.classes <= kWaves * kSome ? 3 : 10) * (uint64_t)s.a.rows;
+    const bool alone = s.a.classes <= 2 * kSome || many;
+    // bf16: 32 classes a lane at a time keep the memory busy (2048 rows of 32768 48.8 -> 46.0 us, 256 rows 18.5 -> 15.8), 16 where those are all that a wave has (one row of
+    // 1000 5.7 -> 4.5, 256 rows of 4096 9.2 -> 7.4) and where workgroups share a row.
+    const bool short_steps = sizeof(T) == 2 && s.a.classes <= (alone ? 1 : kWaves) * kSome;
+    constexpr uint32_t kShort = sizeof(T) == 2 ? 2 : 4;
+    const dim3 rows(s.a.rows), fours((s.a.rows + kWaves - 1) / kWaves), threads(64 * kWaves);
+    if (s.parts > 1) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, true, kShort>), dim3(s.a.rows, s.parts), threads, 0, st, s);
+    else if (short_steps && alone) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false, kShort>), fours, threads, 0, st, s);
+    else if (short_steps) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false, kShort>), rows, threads, 0, st, s);
+    else if (alone) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false, 4>), fours, threads, 0, st, s);
+    else hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false, 4>), rows, threads, 0, st, s);
     return hipGetLastError();
 }
 
