@@ -529,21 +529,22 @@ hipError_t all_rows(ScoreArgs s, hipStream_t st)
 // A row's classes are shared where there are not enough rows to fill the machine: a part leaves at least a chunk to every wave.  Handing over costs some 4 us,
 // and few parts save little (us whole / in parts, 5 alternatives, fp32 and bf16: one row of 16384 10.2 / 10.4 and 9.4 / 10.4, of 24576 12.8 / 10.8 and 10.4 / 10.9, of 65536
 // 22.9 / 10.9 and 18.7 / 10.8; 128 rows of 16384 12.6 / 12.8 and 11.2 / 12.8, of 24576 16.0 / 14.8 and 13.3 / 14.2, of 65536 31.7 / 23.5 and 22.8 / 18.7; 256 rows, in four,
-// of 32768 20.6 / 20.3 and 16.0 / 19.4, of 65536 35.4 / 29.8 and 23.3 / 24.3, of 131072 65.8 / 43.4 and 39.6 / 33.8).
-void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len)
+// of 32768 20.6 / 20.3 and 16.0 / 19.4, of 65536 35.4 / 29.8 and 23.3 / 24.3, of 131072 65.8 / 43.4 and 39.6 / 33.8).  More work in a row pays sooner: with eight given
+// classes 128 rows of 9216 12.6 / 10.1 and 16.3 / 10.0, 256 rows 13.0 / 11.6 and 16.7 / 11.2; with 20 alternatives 256 rows of 32768 30.9 / 21.3 and 23.2 / 20.4.
+void score_split(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top, uint32_t* parts, uint32_t* part_len)
 {
     *parts = 1; *part_len = classes;
     if (rows == 0) return;
     const uint32_t span = kSome * kWaves, spans = (classes + span - 1) / span, want = std::min(kMaxParts, kRecords / rows);
-    if (want < 3 || spans < (want < 8 ? 16u : 5u)) return;
+    if (want < 3 || spans < (n_given >= 4 ? 3u : want >= 8 ? 5u : top > 8 ? 8u : 16u)) return;
     *part_len = (spans + want - 1) / want * span;
     *parts = (uint32_t)(((uint64_t)classes + *part_len - 1) / *part_len);
 }
 
-uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t, uint32_t)
+uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top)
 {
     uint32_t parts, part_len;
-    score_split(rows, classes, &parts, &part_len);
+    score_split(rows, classes, n_given, top, &parts, &part_len);
     return parts > 1 ? kRecords * (4 + sizeof(Part)) : 0;
 }
 

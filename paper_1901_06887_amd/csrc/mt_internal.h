@@ -351,7 +351,7 @@ struct Linear4Shape { uint32_t rt, nt; bool through_lds; };      // tiles of 16 
 Linear4Shape linear4_shape(uint64_t row_tiles, uint32_t most_rows, uint32_t most_k, uint32_t n_cus, uint32_t x_dtype);      // row_tiles: of 16 outputs x 16 rows
 hipError_t prepare_linear4();      // once per device, before the first launch: lets kernels ask for more than 64 KiB of LDS
 hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s);
-void score_split(uint32_t rows, uint32_t classes, uint32_t* parts, uint32_t* part_len);
+void score_split(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top, uint32_t* parts, uint32_t* part_len);
 uint64_t score_scratch_bytes(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top);
 hipError_t launch_score(const ScoreArgs& a, hipStream_t s);
 

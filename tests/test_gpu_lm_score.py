@@ -173,11 +173,12 @@ def test_equal_classes_where_few_come_first(ctx, dtype, rows, classes, few):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("rows,classes", [(1, 16384), (1, 16385), (128, 16385), (147, 20481), (147, 61441), (341, 61441), (342, 61441), (2047, 2049), (2048, 2049), (204, 2049), (205, 2049),
+@pytest.mark.parametrize("rows,classes", [(1, 16384), (1, 16385), (128, 16385), (147, 20481), (147, 61441), (341, 61441), (342, 61441), (341, 8193), (341, 28673), (2047, 2049), (2048, 2049), (204, 2049), (205, 2049),
                                           (2048, 2700)])
 def test_sizes_where_the_work_is_dealt_out_differently(ctx, dtype, rows, classes):
     rng = np.random.default_rng(rows + classes)
-    run(ctx, logits(rng, rows, classes, dtype, scale=1.0), rng.integers(0, classes, (rows, 2)), n=rng.integers(0, classes + 1, rows), top=6)
+    for given, top in ((2, 6), (5, 12)):
+        run(ctx, logits(rng, rows, classes, dtype, scale=1.0), rng.integers(0, classes, (rows, given)), n=rng.integers(0, classes + 1, rows), top=top)
 
 
 @pytest.mark.parametrize("rows", [1, 2, 7, 40, 300, 1500])
