@@ -6,7 +6,7 @@
 #include <new>
 #include <vector>
 
-#include "mt_internal.h"
+#include "lm_internal.h"
 
 using namespace mt;
 

@@ -1,5 +1,6 @@
 // Device helpers shared by the operators behind language models' answers (lm_*.hip).
 #pragma once
+#include "lm_internal.h"
 #include "mt_device.h"
 
 namespace mt {

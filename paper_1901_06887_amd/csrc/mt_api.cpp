@@ -12,7 +12,7 @@
 #include <string>
 #include <vector>
 
-#include "mt_internal.h"
+#include "lm_internal.h"
 #include "../../include/mt_debug.h"
 
 using namespace mt;

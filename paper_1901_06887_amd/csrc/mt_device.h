@@ -27,6 +27,9 @@
 //   small.hip       gather_kernel / gather_image_kernel (submitted rows -> bricks / padded NHWC),
 //                   gap_kernel (global average pooling), head_kernel (softmax + argmax in
 //                   submission order), copy_kernel (the yardstick for byte counters)
+//   lm_norm.hip, lm_linear4.hip, lm_score.hip (helpers of their own: lm_device.h)
+//                   the operators behind language models' answers: residual and norm, layers of 4-bit weights,
+//                   what logits say about given classes
 //
 // A DNN is a fixed sequence of layers applied in turn (paper, section 1.1); a worker
 // hosts many tenants' DNNs and multiplexes their requests (section 3).  The grouping
