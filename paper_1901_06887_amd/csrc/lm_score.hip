@@ -8,6 +8,9 @@
 // them: a value that a quarter of `top` lanes' maxima reach in every wave, so that at least `top` classes do, and few others.  What a wave has in its own
 // list is in order in front of its later classes, so of those an equal one doesn't get in; a list that fills up is cut to its best `top` and raises the bar.
 // One comparison a lane and 16 classes is what that costs where nothing passes.
+//
+// Memory bounds many rows (2048 rows of 32768 fp32 classes, one given and one alternative, 56 us, 4.8 TB/s; without either 48 us, 5.6 TB/s), a chain of memory trips
+// and the fetch of code that runs once few: one row of 1000 4.5 us, 16 masked rows of 65001 with four given and 20 alternatives 16 us, 10 without alternatives.
 #include "lm_device.h"
 
 namespace mt {
