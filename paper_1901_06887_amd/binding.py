@@ -8,7 +8,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -100,12 +99,6 @@ class mt_score_args(ctypes.Structure):
                 [(n, ctypes.c_uint32) for n in ("rows", "classes", "n_given", "top", "dtype")] + [("temperature", ctypes.c_float)])
 
 
-# The same blocks from their values in order, as bytes: a structure filled by name takes several times as long.
-pack_norm_args = struct.Struct("@8P7Q4IfI").pack
-pack_linear4_args = struct.Struct("@3P3Q4I").pack
-pack_score_args = struct.Struct("@10P3Q5If").pack
-
-
 class mt_profile(ctypes.Structure):
     _fields_ = [("batcher_ms", ctypes.c_float), ("gather_ms", ctypes.c_float), ("head_ms", ctypes.c_float),
                 ("fc_ms", ctypes.c_float * MT_MAX_LAYERS), ("fc_big_ms", ctypes.c_float * MT_MAX_LAYERS), ("conv_ms", ctypes.c_float * MT_MAX_LAYERS),
@@ -157,13 +150,12 @@ def load_library() -> ctypes.CDLL:
     L.mt_debug_conv_launch.argtypes = [vp, u32, u32, ctypes.POINTER(u32), ctypes.POINTER(u32), ctypes.POINTER(ctypes.c_uint64)]
     L.mt_set_profiling.argtypes = [vp, ctypes.c_int]
     L.mt_get_profile.argtypes = [vp, ctypes.POINTER(mt_profile)]
-    # (argument blocks go by address: a structure's byref, or the bytes of the pack_..._args functions)
-    L.mt_add_norm.argtypes = [vp, vp, vp]
+    L.mt_add_norm.argtypes = [vp, vp, ctypes.POINTER(mt_norm_args)]
     L.mt_register_matrix4.argtypes = [vp, u32, u32, vp, vp, vp, ctypes.POINTER(u32)]
     L.mt_matrix4_footprint_get.argtypes = [u32, u32, ctypes.POINTER(ctypes.c_uint64)]
     L.mt_unregister_matrix4.argtypes = [vp, u32]
-    L.mt_linear4.argtypes = [vp, vp, vp, ctypes.POINTER(mt_row_group), u32]
-    L.mt_score.argtypes = [vp, vp, vp]
+    L.mt_linear4.argtypes = [vp, vp, ctypes.POINTER(mt_linear4_args), ctypes.POINTER(mt_row_group), u32]
+    L.mt_score.argtypes = [vp, vp, ctypes.POINTER(mt_score_args)]
     L.mt_score_scratch_get.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_uint64)]
     L.mt_last_error.argtypes = [vp]
     L.mt_last_error.restype = ctypes.c_char_p
@@ -353,22 +345,18 @@ class Context:
     def unregister_matrix4(self, matrix: int):
         self._check(self._lib.mt_unregister_matrix4(self._h, matrix))
 
-    # `args` of these three: a structure (mt_norm_args, ...), or the bytes of one (pack_norm_args, ...)
     def add_norm(self, stream_ptr: int, args):
-        st = self._lib.mt_add_norm(self._h, stream_ptr, args if type(args) is bytes else ctypes.addressof(args))
-        if st:
-            self._check(st)
+        st = self._lib.mt_add_norm(self._h, stream_ptr, ctypes.byref(args))
+        self._check(st)
 
     def linear4(self, stream_ptr: int, args, groups):
         """`groups`: a ctypes array of mt_row_group (row_groups)."""
-        st = self._lib.mt_linear4(self._h, stream_ptr, args if type(args) is bytes else ctypes.addressof(args), groups, len(groups))
-        if st:
-            self._check(st)
+        st = self._lib.mt_linear4(self._h, stream_ptr, ctypes.byref(args), groups, len(groups))
+        self._check(st)
 
     def score(self, stream_ptr: int, args):
-        st = self._lib.mt_score(self._h, stream_ptr, args if type(args) is bytes else ctypes.addressof(args))
-        if st:
-            self._check(st)
+        st = self._lib.mt_score(self._h, stream_ptr, ctypes.byref(args))
+        self._check(st)
 
     def stats(self) -> dict:
         s = mt_stats()

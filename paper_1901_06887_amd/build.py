@@ -1,11 +1,13 @@
-"""Compile the HIP sources of the runtime into ``libmt.so`` next to this file (gfx950 only)."""
+"""Compile the HIP sources of the runtime into ``libmt.so`` next to this file (gfx950 only), and the calls on torch tensors into ``_answers.so``."""
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmt.so")
+CALLS = os.path.join(HERE, "_answers.so")
 SOURCES = ["mt_api.cpp", "batcher.hip", "fc_stream.hip", "fc_big.hip", "conv.hip", "conv_first.hip", "small.hip",
            "lm_api.cpp", "lm_norm.hip", "lm_linear4.hip", "lm_score.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
@@ -27,10 +29,28 @@ def compile_one(src: str, verbose: bool) -> str:
     return obj
 
 
+def compile_calls(verbose: bool) -> None:
+    """csrc/lm_torch.cpp: host code, against torch's headers."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-Wall", "-fPIC", "-shared", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+           *("-isystem" + d for d in (os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"])),
+           os.path.join(CSRC, "lm_torch.cpp"), "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-o", CALLS]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("g++ failed for lm_torch.cpp:\n%s" % r.stdout)
+    if r.stdout.strip():
+        print(r.stdout, file=sys.stderr)
+
+
 def build(verbose: bool = False) -> str:
     from concurrent.futures import ThreadPoolExecutor
     with ThreadPoolExecutor(max_workers=min(8, os.cpu_count() or 1)) as pool:       # one hipcc per source
+        calls = pool.submit(compile_calls, verbose)
         objs = list(pool.map(lambda src: compile_one(src, verbose), SOURCES))
+        calls.result()
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     subprocess.check_call(cmd)
     return LIB

@@ -176,8 +176,17 @@ def test_score_refuses():
     c.close()
 
 
-def test_packed_blocks_are_the_structures():
-    """The bytes that the packing functions make are those of the structure filled field by field."""
-    for pack, cls in ((B.pack_norm_args, B.mt_norm_args), (B.pack_linear4_args, B.mt_linear4_args), (B.pack_score_args, B.mt_score_args)):
-        values = [0.5 if t is ctypes.c_float else i + 3 for i, (_, t) in enumerate(cls._fields_)]
-        assert pack(*values) == bytes(cls(*values))
+def test_calls_on_tensors_refuse_what_is_no_tensor_on_the_device():
+    """Without a GPU no call goes through: every operand is looked at before anything is dereferenced."""
+    import torch
+    c = host_ctx()
+    x = torch.zeros(2, 8)
+    calls = mt.torch_io.answers()
+    for f, args in ((calls.add_norm, (x, None, None, None, 1e-6, None, x, None, None)), (calls.add_norm, (3, None, None, None, 1e-6, None, x, None, None)),
+                    (calls.linear4, (mt.row_groups([(0, 0, 2)]), x, x, None, 0)), (calls.linear4, (None, x.half(), x, None, 0)),
+                    (calls.score, (x, None, None, None, 1.0, None, None, x[0], None, None, x)), (calls.score, (x[0], None, None, None, 1.0, None, None, x[0], None, None, x))):
+        with pytest.raises(ValueError):
+            f(c._h.value, 0, 0, *args)
+        with pytest.raises(TypeError):
+            f(c._h.value, 0, 0, *args, None)
+    c.close()
