@@ -19,8 +19,10 @@ constexpr uint64_t kMaxGrid = 0xffffffffu / 512;         // a grid holds fewer t
 #define LM_TRY(c, expr)                                                                                                     \
     do {                                                                                                                    \
         const hipError_t e_ = (expr);                                                                                       \
-        if (e_ != hipSuccess)                                                                                               \
+        if (e_ != hipSuccess) {                                                                                             \
+            (void)hipGetLastError();                                                                                        \
             return ctx_fail((c), e_ == hipErrorOutOfMemory ? MT_ENOMEM : MT_EDEVICE, "%s: %s", #expr, hipGetErrorString(e_)); \
+        }                                                                                                                   \
     } while (0)
 
 inline uint32_t div_up(uint32_t a, uint32_t b) { return (uint32_t)(((uint64_t)a + b - 1) / b); }
@@ -166,10 +168,8 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
     LM_TRY(c, hipSetDevice(v.device));
 
     const Linear4Shape shape = linear4_shape(row_tiles, most_rows, most_k, v.n_cus, a->x_dtype);
-    Linear4Args k;
-    k.arena = v.arena; k.x = a->x; k.x_scales = a->x_scales; k.y = a->y;
-    k.x_stride = a->x_stride; k.x_scales_stride = a->x_scales_stride; k.y_stride = a->y_stride;
-    k.act = a->act; k.n_groups = 0; k.y_bf16 = a->y_dtype == MT_BF16;
+    Linear4Args<kGroups4> k;
+    k.call = Linear4Call{v.arena, a->x, a->x_scales, a->y, a->x_stride, a->x_scales_stride, a->y_stride, a->act, 0, a->y_dtype == MT_BF16 ? 1u : 0u};
     uint64_t grid = 0;
     for (uint32_t g = 0; g < n_groups; ++g) {
         const mt_row_group& r = groups[g];
@@ -177,11 +177,11 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
         const Matrix4& m = (*v.matrices)[r.matrix];
         const uint64_t wgs = (uint64_t)div_up(m.N, kTile4Rows * shape.nt) * div_up(r.n_rows, kTile4Rows * shape.rt);
         if (wgs > kMaxGrid) return ctx_fail(c, MT_EUNSUPPORTED, "group %u takes %llu workgroups", g, (unsigned long long)wgs);
-        if (k.n_groups == kGroups4 || grid + wgs > kMaxGrid) {
+        if (k.call.n_groups == kGroups4 || grid + wgs > kMaxGrid) {
             LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
-            k.n_groups = 0; grid = 0;
+            k.call.n_groups = 0; grid = 0;
         }
-        k.groups[k.n_groups++] = Group4{m.off, m.N, m.K, r.first_row, r.n_rows, (uint32_t)grid};
+        k.groups[k.call.n_groups++] = Group4{m.off, m.N, m.K, r.first_row, r.n_rows, (uint32_t)grid};
         grid += wgs;
     }
     LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));

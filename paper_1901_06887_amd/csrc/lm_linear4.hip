@@ -211,7 +211,7 @@ __device__ __forceinline__ void store4(__bf16* p, const f32x4& v) { *(Any<__bf16
 __device__ __forceinline__ void store4(float* p, const f32x4& v) { *(Any<float>::vec16*)p = __builtin_bit_cast(u32x4, v); }
 
 template <typename Y>
-__device__ __forceinline__ void store_outputs(const Linear4Args& a, uint64_t row, uint32_t n0, uint32_t N, const f32x4& v)
+__device__ __forceinline__ void store_outputs(const Linear4Call& a, uint64_t row, uint32_t n0, uint32_t N, const f32x4& v)
 {
     Y* y = (Y*)a.y + row * a.y_stride + n0;
     if (n0 + 4 <= N) store4(y, v);
@@ -221,7 +221,7 @@ __device__ __forceinline__ void store_outputs(const Linear4Args& a, uint64_t row
 }
 
 // The biases of four outputs, in loads that no branch holds up; past the last output, its own.
-__device__ __forceinline__ f32x4 bias_of(const Linear4Args& a, const Group4& g, uint32_t n0)
+__device__ __forceinline__ f32x4 bias_of(const Linear4Call& a, const Group4& g, uint32_t n0)
 {
     const float* p = (const float*)(a.arena + g.off + matrix4_tiles_bytes(g.N, g.K));
     f32x4 b;
@@ -231,7 +231,7 @@ __device__ __forceinline__ f32x4 bias_of(const Linear4Args& a, const Group4& g, 
 }
 
 // Four outputs of a row of the group: activation and store.
-__device__ __forceinline__ void finish_tile(const Linear4Args& a, const Group4& g, uint32_t n0, uint32_t in_group, f32x4 v)
+__device__ __forceinline__ void finish_tile(const Linear4Call& a, const Group4& g, uint32_t n0, uint32_t in_group, f32x4 v)
 {
     if (in_group >= g.n_rows || n0 >= g.N) return;
     if (a.act == MT_ACT_GELU) {
@@ -244,14 +244,16 @@ __device__ __forceinline__ void finish_tile(const Linear4Args& a, const Group4& 
 
 // A workgroup's group: the last one that starts at or before it.  (What a kernel reads of its arguments is asked for in one go and waited for here: loads
 // where they are used are as many trips to memory one after the other, some 500 clocks each in a launch's first workgroups.)
-__device__ __forceinline__ Group4 group_of(const Linear4Args& a, uint32_t lane)
+template <uint32_t GROUPS>
+__device__ __forceinline__ Group4 group_of(const Linear4Args<GROUPS>& args, uint32_t lane)
 {
-    Group4 g = a.groups[0];
+    const Linear4Call& a = args.call;
+    Group4 g = args.groups[0];
     asm volatile("" :: "s"(a.arena), "s"(a.x), "s"(a.x_scales), "s"(a.y), "s"(a.x_stride), "s"(a.x_scales_stride), "s"(a.y_stride), "s"(a.act), "s"(a.n_groups), "s"(a.y_bf16),
                  "s"(g.off), "s"(g.N), "s"(g.K), "s"(g.row0), "s"(g.n_rows));
     if (a.n_groups > 1) {
-        const bool starts = lane < a.n_groups && a.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
-        g = a.groups[__builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1)];
+        const bool starts = lane < a.n_groups && args.groups[lane < a.n_groups ? lane : 0].wg_base <= blockIdx.x;
+        g = args.groups[__builtin_amdgcn_readfirstlane(__popcll(__ballot(starts)) - 1)];
         asm volatile("" :: "s"(g.off), "s"(g.N), "s"(g.K), "s"(g.row0), "s"(g.n_rows), "s"(g.wg_base));
     }
     return g;
@@ -263,11 +265,12 @@ constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles 
 // for small matrices the launch and two trips to memory: one bf16 row through 4096 x 65536 26.2 us (5.5 TB/s), through 1024 x 1024 3.4 us; 64 tenants of one to
 // four 8-bit rows through 1024 x 1024 9.3 us (3.9 TB/s).  Waves matter more than depth: with registers for two waves a SIMD instead of three and four the last took 10.2,
 // 40 tenants of 64 fp32 rows through 448 x 960 50 instead of 28; 8 or 16 waves to a workgroup, or deeper walks, gave nothing.
-template <Kind KIND, int NT, int DEPTH>
-__global__ void __launch_bounds__(kWaves4 * 64, KIND == kRowsF32 ? 3 : 2) linear4_kernel(Linear4Args a)
+template <Kind KIND, int NT, int DEPTH, uint32_t GROUPS>
+__global__ void __launch_bounds__(kWaves4 * 64, KIND == kRowsF32 ? 3 : 2) linear4_kernel(Linear4Args<GROUPS> args)
 {
+    const Linear4Call& a = args.call;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Group4 g = group_of(a, lane);
+    const Group4 g = group_of(args, lane);
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_slabs = ceil_div(n_tiles, NT);
     const uint32_t local = blockIdx.x - g.wg_base;
@@ -360,7 +363,7 @@ template <Kind KIND, int RT> struct RowFetch {
     uint32_t scale[KIND == kRowsMx8 ? kPasses : 1];
     uint32_t u, row0;              // which load along the row, and row, this thread starts with
 
-    __device__ __forceinline__ RowFetch(const Linear4Args& a, const Group4& g, uint32_t first_row, uint32_t t) : u(t % kAcross), row0(t / kAcross)
+    __device__ __forceinline__ RowFetch(const Linear4Call& a, const Group4& g, uint32_t first_row, uint32_t t) : u(t % kAcross), row0(t / kAcross)
     {
 #pragma unroll
         for (uint32_t i = 0; i < kPasses; ++i) {
@@ -410,13 +413,14 @@ template <Kind KIND, int RT> struct RowFetch {
 };
 
 template <Kind KIND, int RT>
-__global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args a)
+__global__ void __launch_bounds__(512) linear4_rows_kernel(Linear4Args<kGroups4> args)
 {
+    const Linear4Call& a = args.call;
     extern __shared__ __attribute__((aligned(16))) u32x4 lds[];
     constexpr uint32_t kParts = KIND == kRowsF32 ? 3 : 1, kPartVecs = 16 * RT * 16, kTileVecs = kParts * kPartVecs;      // a k tile of the rows, in 16 bytes
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t quarter = wave / kSlabs, li = lane & 15, lq = lane >> 4;
-    const Group4 g = group_of(a, lane);
+    const Group4 g = group_of(args, lane);
     const uint32_t N = g.N, K = g.K;
     const uint32_t n_tiles = ceil_div(N, kTile4Rows), k_tiles = ceil_div(K, kTile4K), n_wide = ceil_div(n_tiles, kNt * kSlabs), chunks = ceil_div(g.n_rows, 16 * RT);
     // workgroups eight apart share an XCD: they take the same outputs of one chunk of rows after the other
@@ -521,21 +525,20 @@ template <Kind KIND, int RT> constexpr uint32_t rows_lds()
 }
 
 template <Kind KIND, int NT, int DEPTH>
-hipError_t go(const Linear4Args& a, uint32_t grid, hipStream_t s)
+hipError_t go(const Linear4Args<kGroups4>& a, uint32_t grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((linear4_kernel<KIND, NT, DEPTH>), dim3(grid), dim3(kWaves4 * 64), 0, s, a);
-    return hipGetLastError();
+    if (a.call.n_groups <= kFewGroups4) return launch(linear4_kernel<KIND, NT, DEPTH, kFewGroups4>, dim3(grid), kWaves4 * 64, 0, s, a);
+    return launch(linear4_kernel<KIND, NT, DEPTH, kGroups4>, dim3(grid), kWaves4 * 64, 0, s, a);
 }
 
 template <Kind KIND, int RT>
-hipError_t go_rows(const Linear4Args& a, uint32_t grid, hipStream_t s)
+hipError_t go_rows(const Linear4Args<kGroups4>& a, uint32_t grid, hipStream_t s)
 {
-    hipLaunchKernelGGL((linear4_rows_kernel<KIND, RT>), dim3(grid), dim3(512), (rows_lds<KIND, RT>()), s, a);
-    return hipGetLastError();
+    return launch(linear4_rows_kernel<KIND, RT>, dim3(grid), 512, rows_lds<KIND, RT>(), s, a);
 }
 
 template <Kind KIND>
-hipError_t choose(const Linear4Args& a, Linear4Shape shape, uint32_t grid, hipStream_t s)
+hipError_t choose(const Linear4Args<kGroups4>& a, Linear4Shape shape, uint32_t grid, hipStream_t s)
 {
     if (!shape.through_lds) return shape.nt == 1 ? go<KIND, 1, KIND == kRowsF32 ? 1 : 4>(a, grid, s) : go<KIND, 4, 1>(a, grid, s);
     if constexpr (KIND == kRowsF32) return go_rows<KIND, 1>(a, grid, s);
@@ -579,7 +582,7 @@ hipError_t prepare_linear4()
     return e == hipSuccess ? prepare_rows<kRowsMx8, 4>() : e;
 }
 
-hipError_t launch_linear4(const Linear4Args& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s)
+hipError_t launch_linear4(const Linear4Args<kGroups4>& a, Linear4Shape shape, uint32_t x_dtype, uint32_t grid, hipStream_t s)
 {
     if (x_dtype == MT_MX8) return choose<kRowsMx8>(a, shape, grid, s);
     return x_dtype == MT_BF16 ? choose<kRowsBf16>(a, shape, grid, s) : choose<kRowsF32>(a, shape, grid, s);

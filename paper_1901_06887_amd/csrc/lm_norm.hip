@@ -163,13 +163,11 @@ hipError_t go(const mt_norm_args& a, bool stream, hipStream_t s)
     const uint32_t grid = MULTI ? a.rows : (a.rows + 3) / 4;
     const uint32_t need = (a.width + kRun * RUNS - 1) / (kRun * RUNS);
     const uint32_t threads = MULTI ? std::min<uint32_t>((need + 63) / 64 * 64, 1024) : 256;
-    if (stream) hipLaunchKernelGGL((norm_kernel<T, MULTI, RUNS, LOOP, true>), dim3(grid), dim3(threads), 0, s, a);
-    else hipLaunchKernelGGL((norm_kernel<T, MULTI, RUNS, LOOP, false>), dim3(grid), dim3(threads), 0, s, a);
-    return hipGetLastError();
+    return launch(stream ? norm_kernel<T, MULTI, RUNS, LOOP, true> : norm_kernel<T, MULTI, RUNS, LOOP, false>, dim3(grid), threads, 0, s, a);
 }
 
 template <typename T>
-hipError_t launch(const mt_norm_args& a, hipStream_t s)
+hipError_t choose(const mt_norm_args& a, hipStream_t s)
 {
     const uint64_t outputs = (uint64_t)a.rows * a.width * ((a.sum ? sizeof(T) : 0) + (a.y ? sizeof(T) : 0) + (a.y8 ? 1 : 0));
     const bool stream = outputs > kStreamBytes;
@@ -185,7 +183,7 @@ hipError_t all_rows(mt_norm_args a, hipStream_t s)
 {
     for (uint32_t left = a.rows;; left -= kRowsAtOnce) {
         a.rows = std::min(left, kRowsAtOnce);
-        const hipError_t e = launch<T>(a, s);
+        const hipError_t e = choose<T>(a, s);
         if (e != hipSuccess || left <= kRowsAtOnce) return e;
         const uint64_t n = kRowsAtOnce;
         a.x = (const T*)a.x + n * a.x_stride;

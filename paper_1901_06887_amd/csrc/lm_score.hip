@@ -489,13 +489,11 @@ hipError_t go(const ScoreArgs& s, hipStream_t st)
     // 1000 5.7 -> 4.5, 256 rows of 4096 9.2 -> 7.4) and where workgroups share a row.
     const bool short_steps = sizeof(T) == 2 && s.a.classes <= (alone ? 1 : kWaves) * kSome;
     constexpr uint32_t kShort = sizeof(T) == 2 ? 2 : 4;
-    const dim3 rows(s.a.rows), fours((s.a.rows + kWaves - 1) / kWaves), threads(64 * kWaves);
-    if (s.parts > 1) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, true, kShort>), dim3(s.a.rows, s.parts), threads, 0, st, s);
-    else if (short_steps && alone) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false, kShort>), fours, threads, 0, st, s);
-    else if (short_steps) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false, kShort>), rows, threads, 0, st, s);
-    else if (alone) hipLaunchKernelGGL((score_kernel<T, TOP, MASK, 1, false, 4>), fours, threads, 0, st, s);
-    else hipLaunchKernelGGL((score_kernel<T, TOP, MASK, kWaves, false, 4>), rows, threads, 0, st, s);
-    return hipGetLastError();
+    const dim3 rows(s.a.rows), fours((s.a.rows + kWaves - 1) / kWaves);
+    constexpr uint32_t threads = 64 * kWaves;
+    if (s.parts > 1) return launch(score_kernel<T, TOP, MASK, kWaves, true, kShort>, dim3(s.a.rows, s.parts), threads, 0, st, s);
+    if (alone) return launch(short_steps ? score_kernel<T, TOP, MASK, 1, false, kShort> : score_kernel<T, TOP, MASK, 1, false, 4>, fours, threads, 0, st, s);
+    return launch(short_steps ? score_kernel<T, TOP, MASK, kWaves, false, kShort> : score_kernel<T, TOP, MASK, kWaves, false, 4>, rows, threads, 0, st, s);
 }
 
 template <typename T>
