@@ -262,6 +262,9 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
     using R = Raw<T, VECS>;
     constexpr uint32_t kPer = R::kPer, kChunk = R::kChunk;
     const mt_score_args& a = s.a;
+    // (asked for in one go: loads where they are used are as many trips to memory one after the other)
+    asm volatile("" :: "s"(a.logits), "s"(a.n_classes), "s"(a.allowed), "s"(a.given), "s"(a.given_ranks), "s"(a.scratch), "s"(a.row_stride), "s"(a.allowed_stride), "s"(a.rows), "s"(a.classes),
+                 "s"(a.n_given), "s"(a.top), "s"(s.exp2_scale), "s"(s.parts), "s"(s.part_len));
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t row = WAVES == 1 ? blockIdx.x * kWaves + wave : blockIdx.x;
     if (row >= a.rows) return;                    // (whole waves, and none where a barrier follows)
