@@ -3,7 +3,7 @@
 // h = x + r, y = h * rsqrt(mean(h^2) + eps) * gain, q = e4m3(y / 2^e) with the least e >= -126 for which no |y| of the
 // 32 values exceeds 448 * 2^e.  A row is read once and stays in registers between the sum of squares and the outputs; a lane
 // holds runs of eight consecutive elements, so a block of 32 is four neighbouring lanes and its maximum two cross-lane moves.  Memory bounds it: 8192 rows of
-// 4096 bf16, residual, sum, norm and 8-bit rows 53.5 us, 5.7 TB/s.  One row of 1024 takes 2.7 us, which is the launch and two trips to memory; 333 rows of 1531 fp32
+// 4096 bf16, residual, sum, norm and 8-bit rows 53.5 us, 5.7 TB/s.  One row of 1024 takes 2.5 us, which is the launch and two trips to memory; 333 rows of 1531 fp32
 // values 5.4 us (1.6 TB/s: rows that start anywhere, and their ends element by element).
 #include "lm_device.h"
 
@@ -123,6 +123,9 @@ __device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uin
 template <typename T, bool MULTI, uint32_t RUNS, bool LOOP, bool STREAM>
 __global__ void __launch_bounds__(MULTI ? 1024 : 256) norm_kernel(mt_norm_args a)
 {
+    // (asked for in one go: loads where they are used are as many trips to memory one after the other; one row of 1024 2.7 -> 2.5 us, many rows are 1 % slower)
+    if constexpr (!STREAM) asm volatile("" :: "s"(a.x), "s"(a.residual), "s"(a.gain), "s"(a.gain_ids), "s"(a.sum), "s"(a.y), "s"(a.y8), "s"(a.y8_scales), "s"(a.x_stride), "s"(a.residual_stride),
+                 "s"(a.gain_stride), "s"(a.rows), "s"(a.width), "s"(a.n_gains), "s"(a.eps));
     const uint32_t threads = MULTI ? blockDim.x : 64, span = threads * kRun;
     const uint32_t t = MULTI ? threadIdx.x : threadIdx.x & 63;
     const uint32_t row = MULTI ? blockIdx.x : blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

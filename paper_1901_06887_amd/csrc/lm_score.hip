@@ -10,7 +10,7 @@
 // One comparison a lane and 16 classes is what that costs where nothing passes.
 //
 // Memory bounds many rows (2048 rows of 32768 fp32 classes, one given and one alternative, 56 us, 4.8 TB/s; without either 48 us, 5.6 TB/s), a chain of memory trips
-// and the fetch of code that runs once few: one row of 1000 4.5 us, 16 masked rows of 65001 with four given and 20 alternatives 16 us, 10 without alternatives.
+// and the fetch of code that runs once few: one row of 1000 4.4 us, 16 masked rows of 65001 with four given and 20 alternatives 16 us, 9 without alternatives.
 #include "lm_device.h"
 
 namespace mt {
