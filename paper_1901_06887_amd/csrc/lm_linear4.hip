@@ -54,7 +54,7 @@ __device__ __forceinline__ void split3_mostly_finite(const u32x4& x, uint32_t (&
         uint32_t p[3][2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            p[0][h] = __builtin_bit_cast(uint32_t, f[2 * i + h]);
+            p[0][h] = x[2 * i + h];               // (not a cast of the element of f: the compiler takes element 0 for every one)
             const float r = f[2 * i + h] - __builtin_bit_cast(float, p[0][h] & 0xffff0000u);
             p[1][h] = __builtin_bit_cast(uint32_t, r);
             p[2][h] = __builtin_bit_cast(uint32_t, r - __builtin_bit_cast(float, p[1][h] & 0xffff0000u));

@@ -85,6 +85,23 @@ def test_sizes(x_kind, y_kind, k, n):
 
 
 @pytest.mark.parametrize("x_kind", ["bf16", "f32", "mx8"])
+@pytest.mark.parametrize("rows,N,K", [(1, 500, 1024), (3, 8192, 1030), (20, 2000, 257), (130, 8192, 1024), (130, 8192, 1100), (40, 8192, 1024)])
+def test_every_bit_of_a_value_arrives(x_kind, rows, N, K):
+    """Matrices of one power of two to an output: no sum rounds, so every output is that column times it, to the last bit."""
+    rng = np.random.default_rng(rows + K)
+    ctx = context()
+    w, at = np.zeros((N, K)), rng.integers(0, K, N)
+    codes, which = np.zeros((N, K + K % 2), dtype=np.uint8), rng.integers(0, 8, N)
+    codes[np.arange(N), at] = np.array([1, 2, 4, 6, 9, 10, 12, 14])[which]                 # +-0.5, 1, 2, 4
+    w[np.arange(N), at] = lm.E2M1[codes[np.arange(N), at]]
+    m = ctx.register_matrix4(N, K, codes[:, 0::2] | codes[:, 1::2] << 4, np.full((N, -(-K // 32)), 127, dtype=np.uint8))
+    x, e, v = rows_in(rng, x_kind, rows, K, K, 0)
+    y = call(ctx, [(m, 0, rows)], x, e, rows, N, "f32", mt.MT_ACT_NONE)
+    assert np.array_equal(y, v[:, at] * w[np.arange(N), at])
+    ctx.close()
+
+
+@pytest.mark.parametrize("x_kind", ["bf16", "f32", "mx8"])
 @pytest.mark.parametrize("lo,hi", [(1, 1), (1, 3), (0, 40), (60, 150)])
 def test_tenants_of_all_sizes_in_one_call(x_kind, lo, hi):
     """More groups than a launch holds, matrices that all differ, rows that belong to nobody, a tenant with two groups."""
