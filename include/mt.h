@@ -398,7 +398,7 @@ mt_status mt_matrix4_footprint_get(uint32_t out_features, uint32_t in_features, 
 mt_status mt_unregister_matrix4(mt_ctx* ctx, uint32_t matrix);
 
 /* y[i][n] = act(bias[n] + sum_k W[n][k] x[i][k]) for the rows i of each group, W and bias those of the group's
- * matrix: one call serves the rows of many tenants.  Products are exact, sums fp32, y is rounded once.
+ * matrix: one call serves the rows of many tenants.  Products are exact (of fp32 rows, bits below 2^-133 are left out), sums fp32, y is rounded once.
  * Columns of y from a matrix's out_features on, and rows in no group, are left as they are.
  * Groups come in the order of their rows and share none; a group of 0 rows is skipped.
  * Errors: MT_EINVAL (null, strides below a matrix's sizes, rows outside 0..rows or out of order), MT_ENOTFOUND (a

@@ -16,7 +16,7 @@ namespace {
 enum Kind { kRowsF32, kRowsBf16, kRowsMx8 };
 constexpr uint32_t row_size(Kind k) { return k == kRowsF32 ? 4 : k == kRowsBf16 ? 2 : 1; }
 
-// fp32 as three bf16 values whose sum it is: the upper halves of what is left.  An infinity or NaN is the first alone.
+// fp32 as three bf16 values whose sum it is: the upper halves of what is left (bf16's smallest is 2^-133: bits below are lost).  An infinity or NaN is the first alone.
 __device__ __forceinline__ void split3(float x, uint32_t (&part)[3])
 {
     const uint32_t b = __builtin_bit_cast(uint32_t, x);
