@@ -554,8 +554,8 @@ hipError_t prepare_rows() { return hipFuncSetAttribute((const void*)linear4_rows
 //   bf16, 24 rows through 4864 x 832 8.4 / 8.7 / 13.0, three tenants of them 14.3 / 9.7 / 13.7; 16 rows through 4096 x 4096 7.2 / 8.2 / 11.9, 24 rows 9.8 / 8.3 / 11.9,
 //   64 18.6 / 8.7 / 18.5, two tenants of those 34.9 / 14.2 / 18.8, four 66.9 / 24.6 / 20.6; 40 tenants of 64 rows through 448 x 960 84 / 17.0 / 20.2; one row through
 //   4096 x 8192 6.2 / 6.7, x 32768 16.7 / 12.8
-//   fp32, 64 rows through 4096 x 4096 40.9 / 18.2 / 18.6, two tenants 76.3 / 30.3 / 18.4; 8 tenants of 64 rows through 1024 x 1024 24.3 / 11.8 / 9.2; one row
-//   through 4096 x 4096 12.0 / 14.3, x 8192 19.1 / 14.8, x 32768 63.2 / 26.5 / 19.9
+//   fp32, 64 rows through 4096 x 4096 40.9 / 18.2 / 18.6, two tenants 76.3 / 30.3 / 18.4; 8 tenants of 64 rows through 1024 x 1024 24.3 / 11.8 / 9.0; one row
+//   through 4096 x 4096 12.0 / 14.3, x 8192 19.1 / 14.8, x 32768 63.2 / 26.5 / 18.4
 // So rows go through LDS where that makes half as many workgroups as there are compute units (fp32, whose every value is split: three quarters, and for few
 // rows too) of two k tiles or more to a wave; else a workgroup takes 64 outputs where workgroups for 16 would be more than the compute units, or four times as many
 // where few rows are read and not split.
