@@ -417,6 +417,11 @@ typedef struct {
 } mt_linear4_args;
 mt_status mt_linear4(mt_ctx* ctx, void* hip_stream, const mt_linear4_args* args, const mt_row_group* groups, uint32_t n_groups);
 
+/* The same for rows that are narrower than their strides (a slice of columns of a wider buffer): MT_EINVAL, and nothing is touched, where a
+ * group with rows has a matrix of more than x_width in_features or y_width out_features. */
+mt_status mt_linear4_within(mt_ctx* ctx, void* hip_stream, const mt_linear4_args* args, const mt_row_group* groups, uint32_t n_groups,
+                            uint32_t x_width, uint32_t y_width);
+
 /* What rows of logits say, with p = softmax(logits / temperature) over a row's allowed classes: those below
  * n_classes[i] (NULL: all; the n_classes of mt_run fits) whose bit of `allowed` is set (bit c % 32 of word c / 32; NULL: all) and
  * whose logit is not -infinity.  Everything is optional but the logits and one output:

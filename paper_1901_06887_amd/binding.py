@@ -155,6 +155,7 @@ def load_library() -> ctypes.CDLL:
     L.mt_matrix4_footprint_get.argtypes = [u32, u32, ctypes.POINTER(ctypes.c_uint64)]
     L.mt_unregister_matrix4.argtypes = [vp, u32]
     L.mt_linear4.argtypes = [vp, vp, ctypes.POINTER(mt_linear4_args), ctypes.POINTER(mt_row_group), u32]
+    L.mt_linear4_within.argtypes = L.mt_linear4.argtypes + [u32, u32]
     L.mt_score.argtypes = [vp, vp, ctypes.POINTER(mt_score_args)]
     L.mt_score_scratch_get.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_uint64)]
     L.mt_last_error.argtypes = [vp]
@@ -163,7 +164,7 @@ def load_library() -> ctypes.CDLL:
     for name in ("mt_create", "mt_destroy", "mt_register_model", "mt_register_model_bn", "mt_unregister_model", "mt_submit",
                  "mt_submit_batch", "mt_run", "mt_run_static", "mt_last_counts", "mt_get_stats", "mt_tenant_account_get", "mt_estimate_run", "mt_prefetch", "mt_cache_stats_get", "mt_admit", "mt_debug_poison", "mt_debug_copy",
                  "mt_set_profiling", "mt_get_profile", "mt_model_footprint_get", "mt_debug_mfma_rate",
-                 "mt_debug_conv_launch", "mt_add_norm", "mt_register_matrix4", "mt_matrix4_footprint_get", "mt_unregister_matrix4", "mt_linear4",
+                 "mt_debug_conv_launch", "mt_add_norm", "mt_register_matrix4", "mt_matrix4_footprint_get", "mt_unregister_matrix4", "mt_linear4", "mt_linear4_within",
                  "mt_score", "mt_score_scratch_get"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L

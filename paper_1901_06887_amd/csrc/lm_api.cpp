@@ -140,6 +140,11 @@ mt_status mt_unregister_matrix4(mt_ctx* c, uint32_t matrix)
 
 mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, const mt_row_group* groups, uint32_t n_groups)
 {
+    return mt_linear4_within(c, hip_stream, a, groups, n_groups, UINT32_MAX, UINT32_MAX);       // (as wide as the strides)
+}
+
+mt_status mt_linear4_within(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, const mt_row_group* groups, uint32_t n_groups, uint32_t x_width, uint32_t y_width)
+{
     if (!c) return MT_EINVAL;
     if (!a || (!groups && n_groups)) return ctx_fail(c, MT_EINVAL, "null arguments or groups");
     const CtxView v = ctx_view(c);
@@ -159,6 +164,8 @@ mt_status mt_linear4(mt_ctx* c, void* hip_stream, const mt_linear4_args* a, cons
             return ctx_fail(c, MT_EINVAL, "group %u: a stride is below the matrix's %u x %u", g, m.N, m.K);
         next = (uint64_t)r.first_row + r.n_rows;
         if (r.n_rows == 0) continue;
+        if (x_width < m.K || y_width < m.N)
+            return ctx_fail(c, MT_EINVAL, "group %u: rows of %u to %u columns are narrower than the matrix's %u x %u", g, x_width, y_width, m.N, m.K);
         most_rows = std::max(most_rows, r.n_rows);
         most_k = std::max(most_k, m.K);
         row_tiles += (uint64_t)div_up(m.N, kTile4Rows) * div_up(r.n_rows, kTile4Rows);

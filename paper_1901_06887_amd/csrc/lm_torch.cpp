@@ -15,7 +15,7 @@
 namespace {
 
 typedef mt_status (*NormCall)(mt_ctx*, void*, const mt_norm_args*);
-typedef mt_status (*LinearCall)(mt_ctx*, void*, const mt_linear4_args*, const mt_row_group*, uint32_t);
+typedef mt_status (*LinearCall)(mt_ctx*, void*, const mt_linear4_args*, const mt_row_group*, uint32_t, uint32_t, uint32_t);
 typedef mt_status (*ScoreCall)(mt_ctx*, void*, const mt_score_args*);
 NormCall norm_call;
 LinearCall linear_call;
@@ -189,17 +189,18 @@ PyObject* linear4(PyObject*, PyObject* const* o, Py_ssize_t n)
             a.x_dtype = dtype_of(x, "rows");
             if (o[6] != Py_None) throw Refused("scales come with 8-bit rows only");
         }
-        // (a matrix may be narrower than the rows: its sizes are checked against the strides, which for one row are the widths)
+        // (a matrix may be narrower than the rows; that none is wider than the tensors, the library checks for every group)
         rows_of(o[4], "x", s.rows, s.width, type, w.device, &a.x, &a.x_stride);
         a.y_dtype = dtype_of(y, "out");
-        rows_of(o[5], "out", s.rows, matrix(y, "out").width, y.scalar_type(), w.device, &a.y, &a.y_stride);
+        const uint32_t y_width = matrix(y, "out").width;
+        rows_of(o[5], "out", s.rows, y_width, y.scalar_type(), w.device, &a.y, &a.y_stride);
         const unsigned long act = PyLong_AsUnsignedLong(o[7]);
         if (PyErr_Occurred()) { PyErr_Clear(); throw Refused("act: one of MT_ACT_... is wanted"); }
         a.act = (uint32_t)std::min<unsigned long>(act, UINT32_MAX);
         Py_buffer groups;
         if (PyObject_GetBuffer(o[3], &groups, PyBUF_SIMPLE) != 0) { PyErr_Clear(); throw Refused("groups: what row_groups makes is wanted"); }
         const bool whole = groups.len % sizeof(mt_row_group) == 0;
-        const long st = whole ? without_gil([&] { return linear_call(w.ctx, w.stream, &a, (const mt_row_group*)groups.buf, (uint32_t)(groups.len / sizeof(mt_row_group))); }) : 0;
+        const long st = whole ? without_gil([&] { return linear_call(w.ctx, w.stream, &a, (const mt_row_group*)groups.buf, (uint32_t)(groups.len / sizeof(mt_row_group)), s.width, y_width); }) : 0;
         PyBuffer_Release(&groups);
         if (!whole) throw Refused("groups: what row_groups makes is wanted");
         return st;
@@ -244,7 +245,7 @@ PyObject* score(PyObject*, PyObject* const* o, Py_ssize_t n)
     });
 }
 
-// The addresses of mt_add_norm, mt_linear4 and mt_score.
+// The addresses of mt_add_norm, mt_linear4_within and mt_score.
 PyObject* bind(PyObject*, PyObject* const* o, Py_ssize_t n)
 {
     return guarded(n, 3, [&] {

@@ -90,7 +90,7 @@ def answers():
             from . import _answers as calls
         except ImportError as e:
             raise ImportError("_answers.so is missing or was built for another torch: build it with `python -m paper_1901_06887_amd.build` (%s)" % e)
-        calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.mt_add_norm, lib.mt_linear4, lib.mt_score)))
+        calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.mt_add_norm, lib.mt_linear4_within, lib.mt_score)))
         _answers = calls
     return _answers
 

@@ -327,3 +327,28 @@ def test_refusals_of_tensors():
         mt.linear4(ctx, one, x, y, act=3)
     assert e.value.status == 5
     ctx.close()
+
+
+def test_slices_narrower_than_their_strides_are_refused():
+    """Columns of wider buffers: a matrix that needs more of them than the slice has neither reads nor writes what lies beside it."""
+    rng = np.random.default_rng(7)
+    ctx = context()
+    codes, scales, w = lm.random_matrix(rng, 8, 64)
+    m = ctx.register_matrix4(8, 64, codes, scales)
+    xs, ys = torch.randn(4, 80, device="cuda"), torch.full((4, 16), 7.0, device="cuda")
+    x8 = torch.zeros(4, 96, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    e8 = torch.full((4, 3), 127, dtype=torch.uint8, device="cuda")
+    one = mt.row_groups([(m, 0, 4)])
+    for x, y, e in ((xs[:, :63], ys[:, :8], None), (xs[:, :64], ys[:, :7], None), (xs[:, :1], ys[:, :1], None), (xs.to(torch.bfloat16)[:, :63], ys[:, :8], None),
+                    (x8[:, :32], ys[:, :8], e8[:, :1]), (x8[:, :63], ys[:, :8], e8[:, :2])):
+        with pytest.raises(mt.MtError) as err:
+            mt.linear4(ctx, one, x, y, x_scales=e)
+        assert err.value.status == 1
+    torch.cuda.synchronize()
+    assert torch.all(ys == 7.0)
+    mt.linear4(ctx, one, xs[:, :64], ys[:, :8])
+    check(ys[:, :8].double().cpu().numpy(), xs[:, :64].double().cpu().numpy(), w, None, mt.MT_ACT_NONE, "f32", "f32")
+    assert torch.all(ys[:, 8:] == 7.0)
+    mt.linear4(ctx, mt.row_groups([(m, 0, 4)]), xs[:, 3:67], ys[:, 8:])
+    check(ys[:, 8:].double().cpu().numpy(), xs[:, 3:67].double().cpu().numpy(), w, None, mt.MT_ACT_NONE, "f32", "f32")
+    ctx.close()

@@ -190,3 +190,19 @@ def test_calls_on_tensors_refuse_what_is_no_tensor_on_the_device():
         with pytest.raises(TypeError):
             f(c._h.value, 0, 0, *args, None)
     c.close()
+
+
+def test_linear4_of_narrow_rows_refuses():
+    """Strides wide enough for the matrix, columns too few: a slice of a padded buffer.  Groups of 0 rows touch nothing."""
+    c = host_ctx()
+    rng = np.random.default_rng(0)
+    m = c.register_matrix4(8, 64, *lm.random_matrix(rng, 8, 64)[:2])
+    wide = c.register_matrix4(9, 65, *lm.random_matrix(rng, 9, 65)[:2])
+    lib = B.load_library()
+    args = linear_args(x_stride=96, y_stride=32)
+    for groups, x_width, y_width, status in (([(m, 0, 10)], 63, 8, 1), ([(m, 0, 10)], 64, 7, 1), ([(m, 0, 10)], 64, 8, 7), ([(m, 0, 5), (wide, 5, 1)], 64, 9, 1),
+                                             ([(m, 0, 5), (wide, 5, 1)], 65, 8, 1), ([(m, 0, 5), (wide, 5, 1)], 65, 9, 7), ([(m, 0, 5), (wide, 5, 0)], 64, 8, 7)):
+        g = mt.row_groups(groups)
+        assert lib.mt_linear4_within(c._h, None, ctypes.byref(args), g, len(g), x_width, y_width) == status, (groups, x_width, y_width)
+    assert lib.mt_linear4_within(None, None, ctypes.byref(args), None, 0, 64, 8) == 1
+    c.close()
