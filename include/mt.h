@@ -435,7 +435,7 @@ mt_status mt_linear4_within(mt_ctx* ctx, void* hip_stream, const mt_linear4_args
  * scratch: DEVICE memory of mt_score_scratch_get's size for the call's sizes, which few rows of many classes share among
  * workgroups; zero before its first use, left ready for the next call (of any sizes that it is large enough for), and
  * used by one call at a time.  NULL where that size is 0.
- * Errors: MT_EINVAL (null, no classes, a stride below the classes, temperature not positive and finite, given without
+ * Errors: MT_EINVAL (null, no classes, a stride below the classes, temperature below 2^-126 or not finite, given without
  * classes, scratch too small, top or n_given beyond their limits), MT_EUNSUPPORTED (dtype), MT_ESTATE, MT_EDEVICE. */
 typedef struct {
     const void* logits;             /* [rows][row_stride], dtype                        */

@@ -1,6 +1,7 @@
 // Host side of the operators behind language models' answers: argument checks, the 4-bit matrices in a context's
 // weight arena, and the grouping of a call's rows into launches.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -222,8 +223,7 @@ mt_status mt_score(mt_ctx* c, void* hip_stream, const mt_score_args* a)
     if (!a->given_logprobs && !a->given_ranks && !a->entropy && !a->top_ids && !a->top_logprobs) return ctx_fail(c, MT_EINVAL, "no output");
     if (a->row_stride < a->classes || (a->allowed && a->allowed_stride < div_up(a->classes, 32)))
         return ctx_fail(c, MT_EINVAL, "a stride is below the %u classes", a->classes);
-    if (!(a->temperature > 0.0f) || !std::isfinite(a->temperature) || !std::isfinite(1.0f / a->temperature))
-        return ctx_fail(c, MT_EINVAL, "temperature is not positive and finite");
+    if (!(a->temperature >= FLT_MIN) || !std::isfinite(a->temperature)) return ctx_fail(c, MT_EINVAL, "temperature is not positive, normal and finite");
     const uint64_t need = score_scratch_bytes(a->rows, a->classes, a->n_given, a->top);
     if (need && (!a->scratch || a->scratch_bytes < need || (uintptr_t)a->scratch % 16))
         return ctx_fail(c, MT_EINVAL, "the call needs %llu bytes of scratch on a 16-byte boundary", (unsigned long long)need);

@@ -309,3 +309,15 @@ def test_refusals_of_tensors(ctx):
     for kw in (dict(n_given=17), dict(top=33)):
         with pytest.raises(mt.MtError):
             mt.alloc_scores(4, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_temperatures_whose_multiples_leave_the_range_are_refused(ctx, dtype):
+    """Below 2^-126 a temperature's reciprocal, or twice of it, is beyond fp32's range or near it: refused, and 2^-126 itself is not."""
+    x = logits(np.random.default_rng(0), 3, 100, dtype)
+    o = mt.alloc_scores(3, 0, 2)
+    for t in (2.0 ** -126 * (1 - 2.0 ** -23), 6e-39, 4e-39, 3e-39, 1e-39):
+        with pytest.raises(mt.MtError) as e:
+            mt.score(ctx, x, o, temperature=t)
+        assert e.value.status == 1, t
+    run(ctx, x, np.array([[0, 99]] * 3), top=5, temperature=2.0 ** -126)

@@ -206,3 +206,12 @@ def test_linear4_of_narrow_rows_refuses():
         assert lib.mt_linear4_within(c._h, None, ctypes.byref(args), g, len(g), x_width, y_width) == status, (groups, x_width, y_width)
     assert lib.mt_linear4_within(None, None, ctypes.byref(args), None, 0, 64, 8) == 1
     c.close()
+
+
+def test_score_refuses_temperatures_below_the_normal_range():
+    c = host_ctx()
+    for t in (2.0 ** -126 * (1 - 2.0 ** -23), 6e-39, 4e-39, 3e-39):
+        refused(1, c.score, 0, score_args(temperature=t))
+    for t in (2.0 ** -126, 3.4e38):
+        refused(7, c.score, 0, score_args(temperature=t))
+    c.close()
