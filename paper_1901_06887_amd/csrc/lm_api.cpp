@@ -232,7 +232,7 @@ mt_status mt_score(mt_ctx* c, void* hip_stream, const mt_score_args* a)
     ScoreArgs k;
     k.a = *a;
     k.inv_t = (float)(1.0 / (double)a->temperature);
-    k.exp2_scale = (float)std::min(2.0 * 1.4426950408889634 / (double)a->temperature, 1e38);
+    k.exp2_scale = (float)(2.0 * 1.4426950408889634 / (double)a->temperature);       // (at 2^-126, the smallest, below 2^128)
     score_split(a->rows, a->classes, a->n_given, a->top, &k.parts, &k.part_len);
     LM_TRY(c, launch_score(k, (hipStream_t)hip_stream));
     return MT_OK;

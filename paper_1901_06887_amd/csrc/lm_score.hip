@@ -1,7 +1,8 @@
 // mt_score: log probabilities and ranks of given classes, entropy and the best alternatives of rows of logits, in one pass over them.
 //
 // With m the largest allowed logit, z = (x - m) / T, S = sum e^z and U = sum z e^z: log p = z - log S and the entropy is log S - U / S, a sum of two
-// terms that are not negative.  (x - m) / 2 is what is worked with: x - m itself can leave fp32's range.  Every lane carries its own m, S and U and
+// terms that are not negative.  (x - m) / 2 is what is worked with: x - m itself can leave fp32's range.  U is kept with log2(e) z, the exponent of two, in the place
+// of z: where e^z is not 0 that is above -150 at every temperature, so no term of U is large.  Every lane carries its own m, S and U and
 // rescales them once per 16 classes; lanes, waves and workgroups are joined at the end.
 //
 // Alternatives: every wave keeps a list in LDS of what can still be among the best `top` of its classes.  The waves' first 1024 classes set a bar for all of
@@ -62,13 +63,16 @@ __device__ __forceinline__ int32_t key_class(uint64_t key) { return (int32_t)(0x
 __device__ __forceinline__ float half_below(float x, float m) { return fmaf(0.5f, x, -0.5f * m); }
 __device__ __forceinline__ float log_prob(float x, float m, float inv_t, float log_s) { return half_below(x, m) * inv_t * 2.0f - log_s; }
 
+// Exponents of two below this count as this: two to them is 0 either way, and 0 times this is no NaN.
+constexpr float kNothing = -1000.0f;
+
 // Maximum and sums of some classes; nothing yet: {kLowest, 0, 0}.
 struct Sums {
     float m, s, u;
     __device__ __forceinline__ void rebase(float to, float scale)
     {
-        const float d = half_below(m, to), f = __builtin_amdgcn_exp2f(d * scale);
-        u = f * fmaf(fmaxf(d, -1e30f), s, u);
+        const float d = half_below(m, to) * scale, f = __builtin_amdgcn_exp2f(d);
+        u = f * fmaf(fmaxf(d, kNothing), s, u);
         s *= f;
         m = to;
     }
@@ -300,10 +304,10 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
         w.sums.rebase(fmaxf(w.sums.m, most), s.exp2_scale);
 #pragma unroll
         for (uint32_t i = 0; i < kPer; ++i) {
-            const float h = half_below(v[i], w.sums.m);
-            const float e = __builtin_amdgcn_exp2f(h * s.exp2_scale);
+            const float h = half_below(v[i], w.sums.m) * s.exp2_scale;
+            const float e = __builtin_amdgcn_exp2f(h);
             w.sums.s += e;
-            w.sums.u = fmaf(fmaxf(h, -1e30f), e, w.sums.u);
+            w.sums.u = fmaf(fmaxf(h, kNothing), e, w.sums.u);
         }
         if (a.given_ranks)
             for (uint32_t g = 0; g < a.n_given; ++g) {
@@ -461,7 +465,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) score_kernel(ScoreArgs s)
     // (the largest logit's own term is 1: without a class the sum is 0, with a NaN or +infinity among them it is NaN)
     const bool some = w.sums.s != 0.0f, lost = some && !(w.sums.s < __builtin_inff());
     const float log_s = logf(w.sums.s), nan = __builtin_nanf("");
-    if (lane == 0 && a.entropy) a.entropy[row] = lost ? nan : some ? log_s - 2.0f * s.inv_t * (w.sums.u / w.sums.s) : 0.0f;
+    if (lane == 0 && a.entropy) a.entropy[row] = lost ? nan : some ? log_s - 0.69314718f * (w.sums.u / w.sums.s) : 0.0f;
     if (lane < a.n_given) {
         const bool there = given_x != kNone;
         const uint64_t to = (uint64_t)row * a.n_given + lane;

@@ -321,3 +321,23 @@ def test_temperatures_whose_multiples_leave_the_range_are_refused(ctx, dtype):
             mt.score(ctx, x, o, temperature=t)
         assert e.value.status == 1, t
     run(ctx, x, np.array([[0, 99]] * 3), top=5, temperature=2.0 ** -126)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("classes", [33, 900, 4100, 40000])
+def test_temperatures_of_the_whole_range(ctx, dtype, classes):
+    """At temperatures of the size of the largest differences these count, however large; at the smallest temperatures the smallest differences do."""
+    rng = np.random.default_rng(classes + 4)
+    x = logits(rng, 8, classes, dtype)
+    x[0, ::2], x[0, 1::2] = LOWEST[dtype], -LOWEST[dtype]          # as far apart as there is
+    x[1] = LOWEST[dtype]
+    x[1, 5] = -LOWEST[dtype]
+    x[2] = -LOWEST[dtype]
+    x[2, 7] = LOWEST[dtype]
+    x[3] = torch.from_numpy(rng.uniform(-3e38, 3e38, classes)).to(DT[dtype])
+    x[4, ::3] = -float("inf")
+    x[5] = torch.from_numpy(rng.integers(-64, 64, classes) * 2.0 ** -130).to(DT[dtype])
+    x[6] = torch.from_numpy(rng.integers(-64, 64, classes) * 2.0 ** -128).to(DT[dtype])
+    given = np.array([[0, 1, 5, 7, classes - 1]] * 8)
+    for temperature in (1e38, 3.4e38, 1e36, 1e30, 1e20, 1e-20, 2e-38, 2.0 ** -126):
+        run(ctx, x, given, top=9, temperature=temperature)
