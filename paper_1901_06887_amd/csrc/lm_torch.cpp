@@ -225,16 +225,18 @@ PyObject* score(PyObject*, PyObject* const* o, Py_ssize_t n)
             rows_of(o[6], "allowed", s.rows, words.width, kInt, w.device, &a.allowed, &a.allowed_stride);
         }
         a.temperature = number(o[7], "temperature");
-        if ((o[4] == Py_None) != (o[9] == Py_None)) throw Refused("given classes and their outputs come together");
+        // (outputs may be left out: how many classes are given, and how many alternatives are wanted, either of a pair says)
+        const auto either = [&](int i, int j) { return o[i] != Py_None ? o[i] : o[j]; };
+        if ((o[4] == Py_None) != (either(8, 9) == Py_None)) throw Refused("given classes and their outputs come together");
         if (o[4] != Py_None) {
-            a.n_given = matrix(tensor(o[9], "given_ranks"), "given_ranks").width;
+            a.n_given = matrix(tensor(either(8, 9), "outputs of given classes"), "outputs of given classes").width;
             table_of(o[4], "given", s.rows, a.n_given, kInt, w.device, &a.given);
             table_of(o[8], "given_logprobs", s.rows, a.n_given, kF32, w.device, &a.given_logprobs);
             table_of(o[9], "given_ranks", s.rows, a.n_given, kInt, w.device, &a.given_ranks);
         }
         list_of(o[10], "entropy", s.rows, kF32, w.device, &a.entropy);
-        if (o[11] != Py_None) {
-            a.top = matrix(tensor(o[11], "top_ids"), "top_ids").width;
+        if (either(11, 12) != Py_None) {
+            a.top = matrix(tensor(either(11, 12), "alternatives"), "alternatives").width;
             table_of(o[11], "top_ids", s.rows, a.top, kInt, w.device, &a.top_ids);
             table_of(o[12], "top_logprobs", s.rows, a.top, kF32, w.device, &a.top_logprobs);
         }

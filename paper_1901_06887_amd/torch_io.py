@@ -118,9 +118,10 @@ def linear4(ctx: B.Context, groups, x: torch.Tensor, out: torch.Tensor, x_scales
 
 @dataclass
 class Scores:
+    """Outputs of mt_score; one that is set to None is left out."""
     given_logprobs: Optional[torch.Tensor]   # float32 [R, n_given]
     given_ranks: Optional[torch.Tensor]      # int32 [R, n_given]
-    entropy: torch.Tensor                    # float32 [R]
+    entropy: Optional[torch.Tensor]          # float32 [R]
     top_ids: Optional[torch.Tensor]          # int32 [R, top]
     top_logprobs: Optional[torch.Tensor]     # float32 [R, top]
     scratch: torch.Tensor                    # uint8: what the workgroups that share a row hand over

@@ -341,3 +341,30 @@ def test_temperatures_of_the_whole_range(ctx, dtype, classes):
     given = np.array([[0, 1, 5, 7, classes - 1]] * 8)
     for temperature in (1e38, 3.4e38, 1e36, 1e30, 1e20, 1e-20, 2e-38, 2.0 ** -126):
         run(ctx, x, given, top=9, temperature=temperature)
+
+
+def test_outputs_on_tensors_alone(ctx):
+    """An output that is None is left out; the others are as they were."""
+    rng = np.random.default_rng(2)
+    x = logits(rng, 4, 5000, "f32")
+    given = torch.from_numpy(rng.integers(0, 5000, (4, 2)).astype(np.int32)).cuda()
+    names = ("given_logprobs", "given_ranks", "entropy", "top_ids", "top_logprobs")
+    full = mt.score(ctx, x, mt.alloc_scores(4, 2, 5), given=given)
+    for kept in [(n,) for n in names] + [("given_logprobs", "top_logprobs"), ("given_ranks", "top_ids"), ("entropy", "top_logprobs")]:
+        o = mt.alloc_scores(4, 2, 5)
+        for n in names:
+            getattr(o, n).fill_(77) if n in kept else setattr(o, n, None)
+        mt.score(ctx, x, o, given=given if any(n.startswith("given") for n in kept) else None)
+        for n in kept:
+            assert torch.equal(getattr(o, n), getattr(full, n)), (kept, n)
+    # outputs without what they are for, or of other sizes than each other
+    for change in (dict(given_logprobs=torch.empty(4, 3, device="cuda")), dict(top_logprobs=torch.empty(4, 6, device="cuda")), dict(given_ranks=None, given_logprobs=None)):
+        o = mt.alloc_scores(4, 2, 5)
+        for n, v in change.items():
+            setattr(o, n, v)
+        with pytest.raises(ValueError):
+            mt.score(ctx, x, o, given=given)
+    o = mt.alloc_scores(4, 2, 5)
+    o.given_ranks = None
+    with pytest.raises(ValueError):
+        mt.score(ctx, x, o)
