@@ -7,6 +7,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <sstream>
 #include <stdexcept>
 
@@ -138,6 +139,18 @@ template <typename F> long without_gil(F f)
     return st;
 }
 
+// Outputs of a call that went through count as changed, so that autograd notices where it had kept one.  (Tensors of inference mode carry no versions.)
+long written(long status, std::initializer_list<PyObject*> outputs)
+{
+    if (status == MT_OK)
+        for (PyObject* o : outputs) {
+            if (o == Py_None) continue;
+            const at::Tensor& t = THPVariable_Unpack(o);
+            if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+        }
+    return status;
+}
+
 // x, residual, gain, gain_ids, eps, sum, y, y8, y8_scales
 PyObject* add_norm(PyObject*, PyObject* const* o, Py_ssize_t n)
 {
@@ -167,7 +180,7 @@ PyObject* add_norm(PyObject*, PyObject* const* o, Py_ssize_t n)
         rows_of(o[9], "out", s.rows, s.width, type, w.device, &a.y, &a.y_stride);
         rows_of(o[10], "out8", s.rows, s.width, kE4m3, w.device, &a.y8, &a.y8_stride);
         rows_of(o[11], "out8_scales", s.rows, ((uint64_t)s.width + 31) / 32, kE8m0, w.device, &a.y8_scales, &a.y8_scales_stride);
-        return without_gil([&] { return norm_call(w.ctx, w.stream, &a); });
+        return written(without_gil([&] { return norm_call(w.ctx, w.stream, &a); }), {o[8], o[9], o[10], o[11]});
     });
 }
 
@@ -203,7 +216,7 @@ PyObject* linear4(PyObject*, PyObject* const* o, Py_ssize_t n)
         const long st = whole ? without_gil([&] { return linear_call(w.ctx, w.stream, &a, (const mt_row_group*)groups.buf, (uint32_t)(groups.len / sizeof(mt_row_group)), s.width, y_width); }) : 0;
         PyBuffer_Release(&groups);
         if (!whole) throw Refused("groups: what row_groups makes is wanted");
-        return st;
+        return written(st, {o[5]});
     });
 }
 
@@ -243,7 +256,7 @@ PyObject* score(PyObject*, PyObject* const* o, Py_ssize_t n)
         const at::Tensor& scratch = tensor(o[13], "scratch");
         list_of(o[13], "scratch", scratch.numel(), at::kByte, w.device, &a.scratch);
         a.scratch_bytes = scratch.numel();
-        return without_gil([&] { return score_call(w.ctx, w.stream, &a); });
+        return written(without_gil([&] { return score_call(w.ctx, w.stream, &a); }), {o[8], o[9], o[10], o[11], o[12], o[13]});
     });
 }
 

@@ -100,7 +100,7 @@ def add_norm(ctx: B.Context, x: torch.Tensor, residual: Optional[torch.Tensor] =
              out8: Optional[torch.Tensor] = None, out8_scales: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """mt_add_norm on the given (or current) stream: h = x + residual into sum_out, h / rms(h) * gain into out (in x's type) and, as
     8-bit rows, into out8 (float8_e4m3fn) and out8_scales (float8_e8m0fnu, or its bytes).  gain: float32 [width], or [tenants, width] with
-    gain_ids int32 [rows]."""
+    gain_ids int32 [rows].  Forward only, like the other operators: inputs may require gradients, no output carries one."""
     st = (_answers or answers()).add_norm(ctx._h.value or 0, stream.cuda_stream if stream is not None else _raw_stream(ctx.device), ctx.device, x, residual, gain, gain_ids,
                                           eps, sum_out, out, out8, out8_scales)
     if st:
@@ -110,7 +110,7 @@ def add_norm(ctx: B.Context, x: torch.Tensor, residual: Optional[torch.Tensor] =
 def linear4(ctx: B.Context, groups, x: torch.Tensor, out: torch.Tensor, x_scales: Optional[torch.Tensor] = None, act: int = B.MT_ACT_NONE,
             stream: Optional[torch.cuda.Stream] = None) -> None:
     """mt_linear4 on the given (or current) stream: the rows of every group (row_groups) times its matrix, into out (float32 or bfloat16).
-    x: float32, bfloat16, or float8_e4m3fn with x_scales."""
+    x: float32, bfloat16, or float8_e4m3fn with x_scales.  Forward only."""
     st = (_answers or answers()).linear4(ctx._h.value or 0, stream.cuda_stream if stream is not None else _raw_stream(ctx.device), ctx.device, groups, x, out, x_scales, act)
     if st:
         ctx._check(st)
@@ -138,7 +138,7 @@ def alloc_scores(rows: int, n_given: int = 0, top: int = 0, device="cuda:0", cla
 def score(ctx: B.Context, logits: torch.Tensor, out: Scores, given: Optional[torch.Tensor] = None, n_classes: Optional[torch.Tensor] = None,
           allowed: Optional[torch.Tensor] = None, temperature: float = 1.0, stream: Optional[torch.cuda.Stream] = None) -> Scores:
     """mt_score on the given (or current) stream: what rows of logits say about given classes (int32 [rows, n_given]), their entropy and
-    the best alternatives.  n_classes: int32 [rows]; allowed: int32 [rows, words], a bit for every class."""
+    the best alternatives.  n_classes: int32 [rows]; allowed: int32 [rows, words], a bit for every class.  Forward only."""
     st = (_answers or answers()).score(ctx._h.value or 0, stream.cuda_stream if stream is not None else _raw_stream(ctx.device), ctx.device, logits, given, n_classes, allowed,
                                        temperature, out.given_logprobs, out.given_ranks, out.entropy, out.top_ids, out.top_logprobs, out.scratch)
     if st:

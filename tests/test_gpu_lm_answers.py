@@ -66,3 +66,28 @@ def test_the_step_of_several_tenants(rows_of, width, hidden, vocabulary):
             bound = ref["bound"] if want.ndim == 1 else ref["bound"][:, None]
             assert np.all(np.abs(in_64(got) - want) <= bound + 2.0 ** -21 * np.abs(want))
     step.close()
+
+
+@pytest.mark.parametrize("what", ["norm", "layer", "scores"])
+def test_written_tensors_count_as_changed(what):
+    """What a graph of gradients has saved may not be overwritten without a word."""
+    import paper_1901_06887_amd as mt
+    ctx = mt.Context(1, 1, 64, 1, 1 << 20, mt.MT_BF16, 0)
+    x, w = torch.randn(4, 32, device="cuda"), torch.ones(4, 32, device="cuda", requires_grad=True)
+    out = torch.ones(4, 32, device="cuda")
+    loss = (w * out).sum()
+    if what == "norm":
+        mt.add_norm(ctx, x, out=out)
+    elif what == "layer":
+        m = ctx.register_matrix4(32, 32, np.full((32, 16), 0x22, dtype=np.uint8), np.full((32, 1), 127, dtype=np.uint8))
+        mt.linear4(ctx, mt.row_groups([(m, 0, 4)]), x, out)
+    else:
+        o = mt.alloc_scores(4, 0, 32)
+        o.top_logprobs = out
+        mt.score(ctx, x, o)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    with torch.inference_mode():            # (tensors that carry no versions)
+        a = torch.ones(4, 32, device="cuda")
+    mt.add_norm(ctx, x, out=a)
+    ctx.close()
