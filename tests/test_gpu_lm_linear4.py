@@ -352,3 +352,30 @@ def test_slices_narrower_than_their_strides_are_refused():
     mt.linear4(ctx, mt.row_groups([(m, 0, 4)]), xs[:, 3:67], ys[:, 8:])
     check(ys[:, 8:].double().cpu().numpy(), xs[:, 3:67].double().cpu().numpy(), w, None, mt.MT_ACT_NONE, "f32", "f32")
     ctx.close()
+
+
+@pytest.mark.parametrize("y_kind", ["bf16", "f32"])
+def test_gelu_of_every_size(y_kind):
+    """Values themselves through a weight of 1.  z Phi(z) changes by (1 + z^2) times a relative change of z, so an error of 2^-24 in an argument of the exponential
+    counts z^2 times: z^2 2^-22 and 2^-19 (bf16: 2^-16) of the result are allowed for, and its rounding."""
+    from math import erfc
+    ctx = context(1 << 20)
+    z = np.concatenate([np.linspace(-14.0, 14.0, 3001), -np.exp2(np.linspace(-100, 3.7, 500)), np.exp2(np.linspace(-100, 100, 500)), [0.0, -0.0, -20.0, -100.0, -1e10, -1e30, 1e30]]).astype(np.float32)
+    m = ctx.register_matrix4(1, 1, np.array([[2]], dtype=np.uint8), np.array([[127]], dtype=np.uint8))
+    y = call(ctx, [(m, 0, len(z))], torch.from_numpy(z[:, None].copy()).cuda(), None, len(z), 1, y_kind, mt.MT_ACT_GELU)[:, 0]
+    z = z.astype(np.float64)
+    ref = np.array([0.5 * v * erfc(-v * 0.5 ** 0.5) for v in z])
+    rel = np.minimum(z * z, 400.0) * 2.0 ** -22 + (2.0 ** -16 + 2.0 ** -8 if y_kind == "bf16" else 2.0 ** -19)
+    assert np.all(np.abs(y - ref) <= rel * np.abs(ref) + (2.0 ** -133 if y_kind == "bf16" else 2.0 ** -146)), (z[np.argmax(np.abs(y - ref) - rel * np.abs(ref))])
+    ctx.close()
+
+
+@pytest.mark.parametrize("y_kind", ["bf16", "f32"])
+def test_gelu_of_infinities_and_nan(y_kind):
+    """As the definition gives it, and the layers of models: -infinity times 0 is NaN."""
+    ctx = context(1 << 20)
+    m = ctx.register_matrix4(1, 1, np.array([[2]], dtype=np.uint8), np.array([[127]], dtype=np.uint8))
+    x = torch.tensor([[float("inf")], [-float("inf")], [float("nan")], [1.0]], device="cuda")
+    y = call(ctx, [(m, 0, 4)], x, None, 4, 1, y_kind, mt.MT_ACT_GELU)[:, 0]
+    assert y[0] == np.inf and np.isnan(y[1]) and np.isnan(y[2]) and abs(y[3] - 0.8413447) < 2.0 ** -8
+    ctx.close()
