@@ -357,7 +357,8 @@ mt_status mt_get_stats(const mt_ctx* ctx, mt_stats* out);
  * 2^(byte - 127); 0xff is NaN); a row's last block may be shorter.  4-bit weights: e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
  * negatives, the sign is bit 3), with scales of the same kind along the fan-in. */
 
-/* h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain, row by row, in fp32, every output rounded once.
+/* h = x + residual; y = h / sqrt(mean(h^2) + eps) * gain, row by row, in fp32, every output rounded once.  Rows of finite h may have any
+ * magnitude, also where h^2 leaves fp32's range.
  *   sum (h), y: in dtype; y8 with y8_scales: 8-bit rows, a block's scale the least power of two (2^-126 at least) at which none
  *   of its values exceeds 448, 1 where all are zero; where one is infinite or NaN the block's scale and values are NaN.
  * sum, y and y8 (with its scales) may each be NULL, not all of them; sum may be x or residual itself (same stride),

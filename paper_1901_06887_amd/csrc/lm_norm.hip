@@ -73,9 +73,12 @@ __device__ __forceinline__ void load_run(const NormRow<T>& r, uint32_t at, uint3
     }
 }
 
+// What h is multiplied by: a power of two, then the rest.  They are apart because together they can leave fp32's range where the outputs do not.
+struct RowScale { float power, rest; };
+
 // Everything behind the mean: the run's sum, norm and 8-bit values.  All lanes of a block come here together.
 template <bool STREAM, typename T>
-__device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uint32_t width, const float (&h)[kRun], float scale)
+__device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uint32_t width, const float (&h)[kRun], RowScale scale)
 {
     const uint32_t n = at >= width ? 0 : width - at < kRun ? width - at : kRun;
     float y[kRun], g[kRun];
@@ -84,7 +87,7 @@ __device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uin
     }
 #pragma unroll
     for (uint32_t i = 0; i < kRun; ++i) {
-        y[i] = h[i] * scale;
+        y[i] = h[i] * scale.power * scale.rest;
         if (r.gain) y[i] *= g[i];
         if (!r.known || i >= n) y[i] = 0.0f;
     }
@@ -118,6 +121,20 @@ __device__ __forceinline__ void finish_run(const NormRow<T>& r, uint32_t at, uin
     if (n && at % MT_MX_BLOCK == 0) r.y8_scales[at / MT_MX_BLOCK] = finite ? (uint8_t)(e + 127) : 0xff;
 }
 
+// Over the threads of a row, of what 0 changes nothing; `part`: LDS of a workgroup that has one row.
+template <bool MULTI, typename F>
+__device__ __forceinline__ uint32_t row_fold(uint32_t v, uint32_t* part, uint32_t t, uint32_t threads, F f)
+{
+    v = wave_fold(v, f);
+    if constexpr (MULTI) {
+        if ((t & 63) == 0) part[t >> 6] = v;
+        __syncthreads();
+        v = 0;
+        for (uint32_t w = 0; w < threads / 64; ++w) v = f(v, part[w]);
+    }
+    return v;
+}
+
 // Workgroups of the threads that a row needs (MULTI), or of four waves with a row each.  A thread holds RUNS runs of its row in registers, run j of thread t
 // at (j * threads + t) * 8.  LOOP: a row that no workgroup holds is read a second time for the outputs.  STREAM: outputs past the caches.
 template <typename T, bool MULTI, uint32_t RUNS, bool LOOP, bool STREAM>
@@ -141,15 +158,39 @@ __global__ void __launch_bounds__(MULTI ? 1024 : 256) norm_kernel(mt_norm_args a
 #pragma unroll
             for (uint32_t i = 0; i < kRun; ++i) squares = fmaf(h[j][i], h[j][i], squares);
     }
-    squares = wave_total(squares);
-    if constexpr (MULTI) {
-        __shared__ float part[16];
-        if ((t & 63) == 0) part[t >> 6] = squares;
-        __syncthreads();
-        squares = 0.0f;
-        for (uint32_t w = 0; w < threads / 64; ++w) squares += part[w];
+    __shared__ __attribute__((aligned(16))) uint32_t part[3][MULTI ? 16 : 1];
+    const auto add = [](uint32_t p, uint32_t q) { return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, p) + __builtin_bit_cast(float, q)); };
+    squares = __builtin_bit_cast(float, row_fold<MULTI>(__builtin_bit_cast(uint32_t, squares), part[0], t, threads, add));
+    RowScale scale{1.0f, 0.0f};
+    // Squares beyond fp32's range, or so small that bits of them that count lie below it (2^24 squares lose 2^-126 together): the row is read once more, and its
+    // values are brought near 1 by a power of two.  An infinity's row stays as it is, and a row of zeros.  (One comparison, whose rare side lies behind the kernel's code;
+    // one row of 1024 2.46 -> 2.53 us.)
+    constexpr uint32_t kLeast = 27u << 23, kInfinity = 0x7f800000u;       // 2^-100
+    const bool fine = __builtin_bit_cast(uint32_t, squares) - kLeast < kInfinity - kLeast;
+    if (__builtin_expect(!fine, 0) && (squares > 1.0f || (squares >= 0.0f && a.eps < 0x1p-100f))) {
+        const auto again = [&](auto of_value) {
+#pragma nounroll
+            for (uint32_t at = t * kRun; at < a.width; at += span) {
+                float v[kRun];
+                load_run(r, at, a.width, v);
+#pragma unroll
+                for (uint32_t i = 0; i < kRun; ++i) of_value(v[i]);
+            }
+        };
+        uint32_t most = 0;
+        again([&](float v) { most = max(most, __builtin_bit_cast(uint32_t, v) & 0x7fffffffu); });
+        most = row_fold<MULTI>(most, part[1], t, threads, [](uint32_t p, uint32_t q) { return p > q ? p : q; });
+        if (most != 0 && most < kInfinity) {
+            int e = (int)(most >> 23) - 127;
+            if (a.eps > 0.0f) e = max(e, ((int)(__builtin_bit_cast(uint32_t, a.eps) >> 23) - 127) >> 1);       // (eps, too, is brought down to 4 at most)
+            scale.power = power(-min(max(e, -126), 126));
+            squares = 0.0f;
+            again([&](float v) { squares = fmaf(v * scale.power, v * scale.power, squares); });
+            squares = __builtin_bit_cast(float, row_fold<MULTI>(__builtin_bit_cast(uint32_t, squares), part[2], t, threads, add));
+        }
     }
-    const float scale = 1.0f / __builtin_sqrtf(squares / (float)a.width + a.eps);
+    // (behind the branch: the gain is asked for with it)
+    scale.rest = 1.0f / __builtin_sqrtf(squares / (float)a.width + a.eps * scale.power * scale.power);
     for (uint32_t base = 0; base < (LOOP ? a.width : 1); base += RUNS * span) {
 #pragma unroll
         for (uint32_t j = 0; j < RUNS; ++j) {

@@ -239,3 +239,47 @@ def test_refusals_of_tensors(ctx):
         assert e.value.status == 1
     with pytest.raises(ValueError):
         mt.add_norm(ctx, x.half(), out=x.half())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("width", [1, 40, 500, 1000, 4096, 9000, 20000])
+@pytest.mark.parametrize("eps", [0.0, 1e-35, 1e-6, 1e30])
+def test_rows_whose_squares_leave_the_range(ctx, dtype, width, eps):
+    """Finite rows of any magnitude: their squares' sum may lie beyond fp32's largest number, or below its smallest."""
+    rng = np.random.default_rng(width)
+    sizes = np.array([1.0, 1e20, 1e38, 3e18, 1e-18, 1e-25, 1e-37, 1e-39, 1.0])
+    rows = len(sizes)
+    v = rng.uniform(0.3, 3.0, (rows, width)) * rng.choice([-1.0, 1.0], (rows, width)) * sizes[:, None]
+    v[8, ::2] *= 1e36
+    v[8, 1::2] *= 1e-36
+    x = torch.from_numpy(v).to(DT[dtype]).cuda()
+    xv = x.double().cpu().numpy()
+    gain, gv = rows_in(rng, 1, width, width, "f32")
+    for residual in (False, True):
+        a = (x.double() * 0.75).to(DT[dtype]) if residual else x
+        r = (x.double() - a.double()).to(DT[dtype]) if residual else None
+        h = a.double().cpu().numpy() + (r.double().cpu().numpy() if residual else 0.0)
+        h = h.astype(np.float32).astype(np.float64)
+        s, y = torch.empty_like(x) if residual else None, torch.empty_like(x)
+        q, e = torch.empty(rows, width, dtype=torch.uint8, device="cuda"), torch.empty(rows, -(-width // 32), dtype=torch.uint8, device="cuda")
+        mt.add_norm(ctx, a, r, gain, eps=eps, sum_out=s, out=y, out8=q.view(torch.float8_e4m3fn), out8_scales=e)
+        if residual:
+            assert torch.equal(s.double().cpu(), torch.from_numpy(h).to(DT[dtype]).double())
+        yv, qv, ev = y.double().cpu().numpy(), q.cpu().numpy(), e.cpu().numpy()
+        check(h, gv, float(np.float32(eps)), dtype, yv)
+        # rows whose every value is below fp32's smallest are zeros, and zeros have the scale 1
+        gone = np.abs(h / np.sqrt((h * h).mean(1, keepdims=True) + float(np.float32(eps))) * gv).max(1) < 2.0 ** -150
+        check(h[~gone], gv, float(np.float32(eps)), dtype, yv[~gone], qv[~gone], ev[~gone])
+        assert np.all(yv[gone] == 0) and np.all(qv[gone] & 127 == 0) and np.all(ev[gone] == 127)
+
+
+def test_zero_rows_and_infinities_without_eps(ctx):
+    """0 / 0 is NaN; an infinity's row stays as with an eps."""
+    x = torch.zeros(3, 600, device="cuda")
+    x[1] = 1e30
+    x[1, 7] = float("inf")
+    x[2, 3] = 1e-44
+    y = torch.empty_like(x)
+    mt.add_norm(ctx, x, eps=0.0, out=y)
+    assert torch.all(torch.isnan(y[0])) and torch.isnan(y[1, 7]) and int((y[1] == 0).sum()) == 599
+    assert int((y[2] == 0).sum()) == 599 and abs(float(y[2, 3]) - 600 ** 0.5) < 1e-4
