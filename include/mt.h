@@ -399,7 +399,8 @@ mt_status mt_matrix4_footprint_get(uint32_t out_features, uint32_t in_features, 
 mt_status mt_unregister_matrix4(mt_ctx* ctx, uint32_t matrix);
 
 /* y[i][n] = act(bias[n] + sum_k W[n][k] x[i][k]) for the rows i of each group, W and bias those of the group's
- * matrix: one call serves the rows of many tenants.  Products are exact (of fp32 rows, bits below 2^-133 are left out), sums fp32, y is rounded once.
+ * matrix: one call serves the rows of many tenants.  Products are exact, sums fp32, y is rounded once.  (Rows are bf16 values on their way: of fp32 rows, and of
+ * 8-bit rows with scales below 2^-124, bits below 2^-133 are left out; 8-bit values beyond 255 * 2^120, which take scales above 2^119, count as infinite.)
  * GELU is z Phi(z) of the sum z, in fp32 within 2^-19 + z^2 2^-22 of itself, for MT_BF16 within 2^-16 + z^2 2^-22 before the rounding; of -infinity it is NaN.
  * Columns of y from a matrix's out_features on, and rows in no group, are left as they are.
  * Groups come in the order of their rows and share none; a group of 0 rows is skipped.

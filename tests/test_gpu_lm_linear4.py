@@ -379,3 +379,33 @@ def test_gelu_of_infinities_and_nan(y_kind):
     y = call(ctx, [(m, 0, 4)], x, None, 4, 1, y_kind, mt.MT_ACT_GELU)[:, 0]
     assert y[0] == np.inf and np.isnan(y[1]) and np.isnan(y[2]) and abs(y[3] - 0.8413447) < 2.0 ** -8
     ctx.close()
+
+
+@pytest.mark.parametrize("n,k", [(64, 32), (4096, 1056)])
+def test_8_bit_rows_of_every_scale(n, k):
+    """Every value at every scale, against weights that bring the product back into fp32's range: exact from 2^-124 to 2^119 (bytes 3 .. 246); at smaller scales bits
+    below 2^-133 are lost, at larger ones what bf16 cannot hold is infinite."""
+    ctx = context()
+    q = np.array([c for c in range(256) if c & 127 != 127], dtype=np.uint8)
+    x8 = np.zeros((len(q), k), dtype=np.uint8)
+    x8[:, 7] = q
+    for weight_scale, bytes_ in ((227, (0, 1, 2, 3, 4, 9)), (127, (60, 127, 190)), (27, (230, 241, 245, 246, 247, 248, 254))):
+        codes = np.zeros((n, k // 2), dtype=np.uint8)
+        codes[:, 3] = (np.arange(n) % 2 * 8 + 2) << 4                 # column 7: 1 and -1
+        m = ctx.register_matrix4(n, k, codes, np.full((n, k // 32), weight_scale, dtype=np.uint8))
+        sign = np.where(np.arange(n) % 2, -1.0, 1.0)
+        for s in bytes_:
+            scales = np.full((len(q), k // 32), 127, dtype=np.uint8)
+            scales[:, 0] = s
+            y = call(ctx, [(m, 0, len(q))], torch.from_numpy(x8).cuda().view(torch.float8_e4m3fn), torch.from_numpy(scales).cuda(), len(q), n, "f32", mt.MT_ACT_NONE)
+            v = lm.e4m3(q) * 2.0 ** (s - 127.0)
+            want = v[:, None] * sign[None, :] * 2.0 ** (weight_scale - 127.0)
+            if s < 3:
+                assert np.all(np.abs(y - want) <= 2.0 ** -133 * 2.0 ** (weight_scale - 127.0)), s
+            elif s < 247:
+                assert np.array_equal(y, want), s
+            else:
+                fits = np.abs(v) <= (2 - 2.0 ** -7) * 2.0 ** 127
+                assert np.array_equal(y[fits], want[fits]) and np.array_equal(y[~fits], np.sign(want[~fits]) * np.inf), s
+        ctx.unregister_matrix4(m)
+    ctx.close()
