@@ -283,3 +283,45 @@ def test_zero_rows_and_infinities_without_eps(ctx):
     mt.add_norm(ctx, x, eps=0.0, out=y)
     assert torch.all(torch.isnan(y[0])) and torch.isnan(y[1, 7]) and int((y[1] == 0).sum()) == 599
     assert int((y[2] == 0).sum()) == 599 and abs(float(y[2, 3]) - 600 ** 0.5) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width,pad", [(15000, 512, 0), (15000, 505, 3), (3000, 4100, 1), (4400, 2048, 8), (1100, 10000, 5), (700, 20000, 0), (700, 20011, 2)])
+@pytest.mark.parametrize("place", [None, "x", "residual"])
+def test_outputs_larger_than_the_caches(ctx, dtype, rows, width, pad, place):
+    """Above 32 MiB of outputs these go past the caches: wide and cut-off runs, rows that are read twice, sums in place."""
+    assert rows * width * 5 > 32 << 20
+    rng = np.random.default_rng(width)
+    g = torch.Generator("cuda").manual_seed(width)
+    wide = lambda t, p, fill: torch.full((rows * (width + p) + 8,), fill, dtype=t, device="cuda")  # noqa: E731
+    rows_of = lambda buf, p: buf[:rows * (width + p)].view(rows, -1)[:, :width]  # noqa: E731
+    buf_x, buf_r, buf_y, buf_q = wide(DT[dtype], pad, 7.0), wide(DT[dtype], pad, 7.0), wide(DT[dtype], 2 * pad, 7.0), wide(torch.uint8, pad, 0xa5)
+    x, r, y, q = rows_of(buf_x, pad), rows_of(buf_r, pad), rows_of(buf_y, 2 * pad), rows_of(buf_q, pad)
+    x.copy_(torch.randn(rows, width, generator=g, device="cuda"))
+    r.copy_(torch.randn(rows, width, generator=g, device="cuda") * 0.3)
+    gain, gv = rows_in(rng, 4, width, width, "f32")
+    ids = torch.from_numpy(rng.integers(0, 4, rows).astype(np.int32)).cuda()
+    n = -(-width // 32)
+    e = torch.full((rows, n), 0xa5, dtype=torch.uint8, device="cuda")
+    h32 = x.float() + r.float()
+    h = x.double() + r.double()
+    kept = {"x": r.clone(), "residual": x.clone()}.get(place)
+    s = {None: torch.full_like(x, 7.0), "x": x, "residual": r}[place]
+    mt.add_norm(ctx, x, r, gain, ids, eps=1e-5, sum_out=s, out=y, out8=q.view(torch.float8_e4m3fn), out8_scales=e)
+    assert torch.equal(s, h32.to(DT[dtype]))
+    if kept is not None:
+        assert torch.equal(r if place == "x" else x, kept)
+    ref = h * torch.rsqrt((h * h).mean(1, keepdim=True) + float(np.float32(1e-5))) * gain.double()[ids.long()]
+    assert bool(((y.double() - ref).abs() <= (HALF_ULP[dtype] + REL) * ref.abs() + 1e-38).all())
+    for buf, p, fill in ((buf_x, pad, 7.0), (buf_r, pad, 7.0), (buf_y, 2 * pad, 7.0), (buf_q, pad, 0xa5)):
+        assert bool((buf[:rows * (width + p)].view(rows, -1)[:, width:] == fill).all()) and bool((buf[rows * (width + p):] == fill).all())
+    some = np.unique(np.concatenate([[0, 1, rows - 2, rows - 1], rng.integers(0, rows, 60)]))
+    at = torch.from_numpy(some).cuda()
+    check(h[at].cpu().numpy(), gv[ids[at].cpu().numpy()], 1e-5, dtype, None, q[at].cpu().numpy(), e[at].cpu().numpy())
+    # and the 8-bit rows are those of calls of a few rows
+    for first in (0, rows // 2, rows - 9):
+        few = slice(first, first + 9)
+        q1, e1 = torch.empty(9, width, dtype=torch.uint8, device="cuda"), torch.empty(9, n, dtype=torch.uint8, device="cuda")
+        if place is None:
+            mt.add_norm(ctx, x[few], r[few], gain, ids[few], eps=1e-5, out8=q1.view(torch.float8_e4m3fn), out8_scales=e1)
+            assert torch.equal(q[few], q1) and torch.equal(e[few], e1)
