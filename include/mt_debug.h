@@ -83,6 +83,11 @@ uint32_t mt_debug_conv_frame_ahead(uint32_t max_tenants, uint32_t channel_blocks
  * Errors: MT_EINVAL (null context, layer out of range, zero rows), MT_ENOTFOUND (requests of a tenant without a model). */
 mt_status mt_debug_conv_launch(mt_ctx* ctx, uint32_t layer, uint32_t rows, const uint32_t* counts, uint32_t* split, uint64_t* workgroups);
 
+/* Measurement and test aid: how mt_linear4 serves a call of so many tiles of 16 outputs x 16 rows (over its groups, ends counted whole), with most_rows rows
+ * in its largest group and fan-ins of up to most_k, on a device of compute_units: *outputs and *rows of a workgroup.  Returns 1 if rows go through LDS, else 0.
+ * Pure function of its arguments; needs no context and no device. */
+int mt_debug_linear4_shape(uint64_t tiles, uint32_t most_rows, uint32_t most_k, uint32_t compute_units, uint32_t x_dtype, uint32_t* outputs, uint32_t* rows);
+
 /* Measurement aid: what a loop of nothing but bf16 matrix instructions sustains on the current
  * device.  Runs, on `stream`, a kernel in which every wavefront issues v_mfma_f32_32x32x16_bf16
  * on pseudo-random operands (eight independent accumulators, two wavefronts per SIMD, no memory

@@ -157,6 +157,7 @@ def load_library() -> ctypes.CDLL:
     L.mt_linear4.argtypes = [vp, vp, ctypes.POINTER(mt_linear4_args), ctypes.POINTER(mt_row_group), u32]
     L.mt_linear4_within.argtypes = L.mt_linear4.argtypes + [u32, u32]
     L.mt_score.argtypes = [vp, vp, ctypes.POINTER(mt_score_args)]
+    L.mt_debug_linear4_shape.argtypes = [ctypes.c_uint64, u32, u32, u32, u32, ctypes.POINTER(u32), ctypes.POINTER(u32)]
     L.mt_score_scratch_get.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_uint64)]
     L.mt_last_error.argtypes = [vp]
     L.mt_last_error.restype = ctypes.c_char_p
@@ -165,7 +166,7 @@ def load_library() -> ctypes.CDLL:
                  "mt_submit_batch", "mt_run", "mt_run_static", "mt_last_counts", "mt_get_stats", "mt_tenant_account_get", "mt_estimate_run", "mt_prefetch", "mt_cache_stats_get", "mt_admit", "mt_debug_poison", "mt_debug_copy",
                  "mt_set_profiling", "mt_get_profile", "mt_model_footprint_get", "mt_debug_mfma_rate",
                  "mt_debug_conv_launch", "mt_add_norm", "mt_register_matrix4", "mt_matrix4_footprint_get", "mt_unregister_matrix4", "mt_linear4", "mt_linear4_within",
-                 "mt_score", "mt_score_scratch_get"):
+                 "mt_score", "mt_score_scratch_get", "mt_debug_linear4_shape"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -438,6 +439,15 @@ def debug_conv_row_tiling(in_h: int, in_w: int, in_channels: int, ksize: int = 3
                                                    ctypes.byref(n_oh), ctypes.byref(ni), ctypes.byref(tpi), ctypes.byref(frame)):
         return None
     return {"rows_per_tile": n_oh.value, "images_per_tile": ni.value, "tiles_per_image": tpi.value, "frame_bytes": frame.value}
+
+
+def debug_linear4_shape(groups: Sequence, compute_units: int, x_dtype: int) -> dict:
+    """How mt_linear4 serves groups of (rows, out_features, in_features): outputs and rows of a workgroup, and whether rows go through LDS."""
+    there = [g for g in groups if g[0]]
+    outputs, rows = ctypes.c_uint32(), ctypes.c_uint32()
+    lds = load_library().mt_debug_linear4_shape(sum(-(-r // 16) * -(-n // 16) for r, n, _ in there), max(r for r, _, _ in there), max(k for _, _, k in there), compute_units, x_dtype,
+                                                ctypes.byref(outputs), ctypes.byref(rows))
+    return {"outputs": outputs.value, "rows": rows.value, "through_lds": bool(lds)}
 
 
 def version() -> str:

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "lm_internal.h"
+#include "../../include/mt_debug.h"
 
 using namespace mt;
 
@@ -194,6 +195,14 @@ mt_status mt_linear4_within(mt_ctx* c, void* hip_stream, const mt_linear4_args* 
     }
     LM_TRY(c, launch_linear4(k, shape, a->x_dtype, (uint32_t)grid, (hipStream_t)hip_stream));
     return MT_OK;
+}
+
+int mt_debug_linear4_shape(uint64_t tiles, uint32_t most_rows, uint32_t most_k, uint32_t compute_units, uint32_t x_dtype, uint32_t* outputs, uint32_t* rows)
+{
+    const Linear4Shape s = linear4_shape(tiles, most_rows, most_k, compute_units, x_dtype);
+    if (outputs) *outputs = s.nt * kTile4Rows;
+    if (rows) *rows = s.rt * kTile4Rows;
+    return s.through_lds ? 1 : 0;
 }
 
 mt_status mt_score_scratch_get(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top, uint64_t* bytes)

@@ -409,3 +409,124 @@ def test_8_bit_rows_of_every_scale(n, k):
                 assert np.array_equal(y[fits], want[fits]) and np.array_equal(y[~fits], np.sign(want[~fits]) * np.inf), s
         ctx.unregister_matrix4(m)
     ctx.close()
+
+
+# ---- rows through LDS -----------------------------------------------------------------------------
+KIND = {"f32": mt.MT_F32, "bf16": mt.MT_BF16, "mx8": mt.MT_MX8}
+# (rows, out_features, in_features) of every tenant: ends of outputs of every kind, workgroups' outputs that are no multiple of eight, fan-ins of less than a vector, than a tile,
+# than a round of four, whole and not; in the second set also rows in several chunks
+LDS_SETS = {
+    "few rows": [(24, 2064, 1100), (32, 2061, 1152), (17, 2100, 1024), (31, 2070, 1537), (0, 50, 300), (32, 2048, 1030), (1, 2077, 100), (30, 2064, 5), (29, 2063, 640), (25, 2050, 1283), (20, 130, 127), (32, 2300, 1),
+                 (26, 2064, 1025)],
+    "many rows": [(64, 2600, 1100), (50, 2609, 1152), (150, 2603, 1029), (64, 2563, 100), (63, 2600, 5), (1, 2600, 1536), (49, 2690, 1024), (60, 2561, 1283), (2, 17, 300), (64, 2600, 1)],
+}
+
+
+def lds_form(groups, x_kind):
+    """That the call takes rows through LDS, and the rows of a workgroup."""
+    s = mt.debug_linear4_shape(groups, torch.cuda.get_device_properties(0).multi_processor_count, KIND[x_kind])
+    assert s["through_lds"] and s["outputs"] == 128, s
+    return s["rows"]
+
+
+@pytest.fixture(scope="module", params=list(LDS_SETS))
+def lds_set(request):
+    """(groups' sizes, context, numbers, (weights, biases), first rows, rows) of a set; every other matrix has biases."""
+    rng = np.random.default_rng(len(request.param))
+    ctx = context(128 << 20)
+    numbers, values, first, at = [], [], [], 3
+    for i, (rows, n, k) in enumerate(LDS_SETS[request.param]):
+        codes, scales, w = lm.random_matrix(rng, n, k)
+        bias = rng.standard_normal(n).astype(np.float32) if i % 2 == 0 else None
+        numbers.append(ctx.register_matrix4(n, k, codes, scales, bias))
+        values.append((w, bias))
+        first.append(at)
+        at += rows + i % 2                       # (every other group is followed by a row of nobody)
+    yield LDS_SETS[request.param], ctx, numbers, values, first, at
+    ctx.close()
+
+
+@pytest.mark.parametrize("x_kind", ["bf16", "f32", "mx8"])
+@pytest.mark.parametrize("y_kind", ["bf16", "f32"])
+@pytest.mark.parametrize("act", [mt.MT_ACT_NONE, mt.MT_ACT_RELU, mt.MT_ACT_GELU])
+def test_groups_whose_rows_go_through_lds(lds_set, x_kind, y_kind, act):
+    sizes, ctx, numbers, values, first, total = lds_set
+    rng = np.random.default_rng(act)
+    assert lds_form(sizes, x_kind) == (16 if x_kind == "f32" else 32 if max(r for r, _, _ in sizes) <= 32 else 64)
+    x, e, v = rows_in(rng, x_kind, total, 1537, 1537 + 3 * act, act)
+    stride = 2700
+    buf = torch.full((total * stride + 8,), 7.0, dtype=DT[y_kind], device="cuda")
+    y = buf[:total * stride].view(total, stride)
+    mt.linear4(ctx, mt.row_groups(zip(numbers, first, [s[0] for s in sizes])), x, y[:, :2690], x_scales=e, act=act)
+    y = y.double().cpu().numpy()
+    of_somebody = np.zeros(total, dtype=bool)
+    for (rows, n, k), (w, bias), at in zip(sizes, values, first):
+        assert np.all(y[at:at + rows, n:] == 7.0)
+        of_somebody[at:at + rows] = True
+        some = at + np.unique(np.concatenate([[0, rows - 1, rows // 2], rng.integers(0, rows, 5)])) if rows else []
+        if rows:
+            check(y[some, :n], v[some, :k], w, bias, act, x_kind, y_kind)
+    assert np.all(y[~of_somebody] == 7.0) and bool((buf[total * stride:] == 7.0).all())
+
+
+@pytest.mark.parametrize("x_kind", ["bf16", "f32", "mx8"])
+def test_rows_through_lds_whatever_else_is_in_the_call(lds_set, x_kind):
+    """A row's sums are the same bits with and without other groups, as long as rows go through LDS."""
+    sizes, ctx, numbers, _, first, total = lds_set
+    x, e, _ = rows_in(np.random.default_rng(1), x_kind, total, 1537, 1540)
+    whole = torch.zeros(total, 2690, device="cuda")
+    groups = list(zip(numbers, first, [s[0] for s in sizes]))
+    mt.linear4(ctx, mt.row_groups(groups), x, whole, x_scales=e)
+    tried = 0
+    for left_out in ([1], [0, 4], [2, 7, 8]):
+        kept = [i for i in range(len(sizes)) if i not in left_out]
+        try:
+            lds_form([sizes[i] for i in kept], x_kind)
+        except AssertionError:
+            continue
+        tried += 1
+        some = torch.zeros_like(whole)
+        mt.linear4(ctx, mt.row_groups([groups[i] for i in kept]), x, some, x_scales=e)
+        for i, (m, at, rows) in enumerate(groups):
+            assert torch.equal(some[at:at + rows], whole[at:at + rows] if i in kept else torch.zeros_like(whole[at:at + rows])), (left_out, i)
+    assert tried
+
+
+@pytest.mark.parametrize("x_kind", ["bf16", "f32", "mx8"])
+@pytest.mark.parametrize("y_kind", ["bf16", "f32"])
+def test_infinities_and_nan_through_lds(lds_set, x_kind, y_kind):
+    """They stay in their rows, beside numbers of every size in the same vectors; in whole tiles of the fan-in and in the last."""
+    sizes, ctx, numbers, values, first, total = lds_set
+    lds_form(sizes, x_kind)
+    groups = mt.row_groups(zip(numbers, first, [s[0] for s in sizes]))
+    x, e, v = rows_in(np.random.default_rng(2), x_kind, total, 1537, 1537)
+    rows, n, k = sizes[0]                        # (k = 1100: its last tile is not whole)
+    (w, bias), at = values[0], first[0]
+    bad = {}
+    for i, col in enumerate((7, 511, 1023, 1024, 1090, k - 1)):
+        if x_kind == "mx8":
+            x.view(torch.uint8)[at + 2 * i, col] = 127
+            e.view(torch.uint8)[at + 2 * i + 1, col // 32] = 255
+            bad[at + 2 * i] = bad[at + 2 * i + 1] = None
+        else:
+            what = (float("inf"), -float("inf"))[i % 2]
+            x[at + 2 * i, col] = float("nan")
+            x[at + 2 * i + 1, col] = what
+            bad[at + 2 * i], bad[at + 2 * i + 1] = None, (col, what)
+            x[at + 2 * i + 1, col - 1] = 3.0e38 if i % 2 else 1.0e-38        # (beside an infinity neither counts)
+    for act in (mt.MT_ACT_NONE, mt.MT_ACT_RELU, mt.MT_ACT_GELU):
+        y = torch.zeros(total, 2690, dtype=DT[y_kind], device="cuda")
+        mt.linear4(ctx, groups, x, y, x_scales=e, act=act)
+        y = y.double().cpu().numpy()
+        for r, why in bad.items():
+            if why is None:
+                assert np.all(np.isnan(y[r, :n])), (act, r)
+                continue
+            with np.errstate(invalid="ignore"):
+                z = w[:, why[0]] * why[1]        # (0 times infinity is NaN)
+                want = {mt.MT_ACT_NONE: z, mt.MT_ACT_RELU: np.where(z < 0, 0.0, z), mt.MT_ACT_GELU: np.where(z == -np.inf, np.nan, z)}[act]
+            assert np.array_equal(y[r, :n], want, equal_nan=True), (act, r)
+        for (rows_g, n_g, k_g), (w_g, b_g), at_g in zip(sizes, values, first):
+            good = [r for r in range(at_g, at_g + rows_g) if r not in bad][:6]
+            if good:
+                check(y[good, :n_g], v[good, :k_g], w_g, b_g, act, x_kind, y_kind)

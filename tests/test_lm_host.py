@@ -215,3 +215,12 @@ def test_score_refuses_temperatures_below_the_normal_range():
     for t in (2.0 ** -126, 3.4e38):
         refused(7, c.score, 0, score_args(temperature=t))
     c.close()
+
+
+def test_forms_of_linear4_by_sizes():
+    """The rule on 256 compute units, on both sides of its lines: (rows, out, in) of every group; outputs and rows of a workgroup, rows through LDS."""
+    for kind, groups, want in ((B.MT_BF16, [(1, 1024, 1024)], (16, 16, False)), (B.MT_BF16, [(1, 65536, 4096)], (64, 16, False)), (B.MT_BF16, [(512, 4096, 4096)], (128, 64, True)),
+                               (B.MT_MX8, [(50, 4096, 4096)] * 8, (128, 64, True)), (B.MT_BF16, [(64, 4096, 4096)] * 4, (128, 64, True)), (B.MT_BF16, [(64, 4096, 4096)] * 3, (64, 16, False)),
+                               (B.MT_BF16, [(24, 2064, 1100)] * 8, (128, 32, True)), (B.MT_BF16, [(16, 2064, 1100)] * 16, (64, 16, False)), (B.MT_F32, [(16, 2064, 1100)] * 16, (128, 16, True)),
+                               (B.MT_F32, [(64, 4096, 1023)] * 2, (64, 16, False)), (B.MT_F32, [(64, 4096, 1024)] * 2, (128, 16, True)), (B.MT_F32, [(0, 4096, 4096), (1, 100, 64)], (16, 16, False))):
+        assert mt.debug_linear4_shape(groups, 256, kind) == dict(zip(("outputs", "rows", "through_lds"), want)), (kind, groups)
