@@ -265,7 +265,7 @@ constexpr int kWaves4 = 4;      // waves of a workgroup: they share the k tiles 
 
 // A workgroup serves 16 NT outputs of 16 rows of a group; a wave asks for DEPTH k tiles at a time, the next ones before it multiplies.  The weights' bytes bound it,
 // for small matrices the launch and two trips to memory: one bf16 row through 4096 x 65536 26.2 us (5.5 TB/s), through 1024 x 1024 3.4 us; 64 tenants of one to
-// four 8-bit rows through 1024 x 1024 9.3 us (3.9 TB/s).  Waves matter more than depth: with registers for two waves a SIMD instead of three and four the last took 10.2,
+// four 8-bit rows through 1024 x 1024 9.1 us (4.0 TB/s).  Waves matter more than depth: with registers for two waves a SIMD instead of three and four the last took 10.2,
 // 40 tenants of 64 fp32 rows through 448 x 960 50 instead of 28; 8 or 16 waves to a workgroup, or deeper walks, gave nothing.
 template <Kind KIND, int NT, int DEPTH, uint32_t GROUPS>
 __global__ void __launch_bounds__(kWaves4 * 64, KIND == kRowsF32 ? 3 : 2) linear4_kernel(Linear4Args<GROUPS> args)
@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kWaves4 * 64, KIND == kRowsF32 ? 3 : 2) linear
 // together, 16 bytes a lane along the rows (read in place by operands, a load would touch 64 lines; 512 rows through 4096 x 4096 took 44.6 us that way), and
 // put them into LDS as bf16 operands: chunk c (eight values) of row i at slot i ^ c of its sixteen, so that neither the stores along a row nor the loads
 // down the rows meet in a bank.  Two buffers, so one barrier for a k tile.  The weights go from memory to registers two k tiles ahead.
-// 512 bf16 rows through 4096 x 4096 21.5 us (0.80 PFLOP/s), eight tenants of 37 to 64 8-bit rows through 4096 x 4096 with GELU 24.8 us.  Of the latter's 50 thousand clocks
+// 512 bf16 rows through 4096 x 4096 21.5 us (0.80 PFLOP/s), eight tenants of 37 to 64 8-bit rows through 4096 x 4096 with GELU 24.6 us.  Of the latter's 50 thousand clocks
 // 7 pass before the first product (arguments, then rows and weights), 33 in eight rounds of four k tiles, half of them MFMAs (the rest: conversion of the weights, which
 // every wave does for its 64 outputs, LDS stores, the barrier), 10 at the join and the activation.
 constexpr int kSlabs = 2, kQuarters = 4, kNt = 4;

@@ -4,7 +4,7 @@
 // 32 values exceeds 448 * 2^e.  A row is read once and stays in registers between the sum of squares and the outputs; a lane
 // holds runs of eight consecutive elements, so a block of 32 is four neighbouring lanes and its maximum two cross-lane moves.  Memory bounds it: 8192 rows of
 // 4096 bf16, residual, sum, norm and 8-bit rows 53.5 us, 5.7 TB/s.  One row of 1024 takes 2.5 us, which is the launch and two trips to memory; 333 rows of 1531 fp32
-// values 5.4 us (1.6 TB/s: rows that start anywhere, and their ends element by element).
+// values 5.1 us (1.7 TB/s: rows that start anywhere, and their ends element by element).
 #include "lm_device.h"
 
 namespace mt {
