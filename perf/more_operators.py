@@ -363,7 +363,7 @@ def _plain_grow(c, T, ids, tokens):
     fits = need <= c.table.shape[1]
     takes = torch.where(fits, need - have, 0)
     free = torch.nonzero(c.refs == 0).squeeze(1)
-    fits = fits & (takes.cumsum(0) <= free.shape[0])
+    fits = fits & ((takes == 0) | (takes.cumsum(0) <= free.shape[0]))
     i = torch.arange(c.table.shape[1], device="cuda")
     sel = (i >= have.unsqueeze(1)) & (i < need.unsqueeze(1)) & fits.unsqueeze(1)
     table = c.table[ids]
@@ -378,7 +378,7 @@ def _plain_fork(c, T, parents, children):
     was, table = c.lengths[parents], c.table[parents]
     full, part = was // T, was % T > 0
     free = torch.nonzero(c.refs == 0).squeeze(1)
-    fits = (c.lengths[children] == 0) & (part.cumsum(0) <= free.shape[0])
+    fits = (c.lengths[children] == 0) & (~part | (part.cumsum(0) <= free.shape[0]))
     i = torch.arange(table.shape[1], device="cuda")
     shared = (i < full.unsqueeze(1)) & fits.unsqueeze(1)
     pages = table[shared].long()
@@ -432,7 +432,7 @@ def _plain_sample(s, case):
     x, ids = torch.sort(x, dim=1, descending=True, stable=True)
     z = (x.double() - x[:, :1].double()) / torch.where(t > 0, t, 1.0)
     w = torch.where((t > 0) | (j == 0), torch.exp(z), 0.0)            # in the order of falling logits
-    keep = (x > none) & ((j < top_k) | (top_k <= 0)) & (w >= min_p) & ((t > 0) | (j == 0))
+    keep = (x > none) & ((j < top_k) | (top_k <= 0)) & (w >= min_p.clamp(max=1)) & ((t > 0) | (j == 0))
     w = torch.where(keep, w, 0.0)
     sums = w.cumsum(1)
     keep = keep & ((sums - w < top_p * sums[:, -1:]) | (top_p >= 1) | (j == 0))
