@@ -58,7 +58,8 @@ typedef enum {
 typedef enum { MT_FC = 0, MT_CONV2D = 1, MT_GAP = 2, MT_MAXPOOL = 3, MT_ADD = 4 } mt_kind;
 typedef enum { MT_ACT_NONE = 0, MT_ACT_RELU = 1, MT_ACT_GELU = 2 } mt_act;
 typedef enum { MT_F32 = 0, MT_BF16 = 1,
-               MT_MX8 = 2        /* rows of mt_linear4 only: e4m3 values with an e8m0 scale for every MT_MX_BLOCK of a row */
+               MT_MX8 = 2,       /* rows of mt_linear4 only: e4m3 values with an e8m0 scale for every MT_MX_BLOCK of a row */
+               MT_KV8 = 3        /* caches (mt_kv_cache) only: e4m3 values with an e8m0 scale for every token and head      */
 } mt_dtype;
 
 #define MT_MAX_LAYERS 48
@@ -459,6 +460,142 @@ typedef struct {
 } mt_score_args;
 mt_status mt_score(mt_ctx* ctx, void* hip_stream, const mt_score_args* args);
 mt_status mt_score_scratch_get(uint32_t rows, uint32_t classes, uint32_t n_given, uint32_t top, uint64_t* bytes);
+
+/* ---- Caches of language models ---------------------------------------------------------------
+ * Keys and values of the tokens that tenants' sequences have seen, in pages of a few tokens: mt_kv_write puts new tokens'
+ * into their places, mt_attend lets new tokens attend to all of their sequence, the mt_kv_ calls on pages give, share, take back and
+ * move them, and mt_sample chooses the token that comes next.  Conventions as above: DEVICE pointers (argument blocks and this struct are HOST memory),
+ * nothing is allocated or waited for, every call may be captured, and what it decides from lengths and tables it decides on the device.
+ *
+ * Sequence s has lengths[s] tokens; its token t is slot t % page_tokens of page table[s][t / page_tokens].  So it holds its table's first
+ * ceil(lengths[s] / page_tokens) entries, and only they are looked at.  refs[p] counts the sequences that hold page p: 0 is free.  A cache starts with
+ * lengths and refs of 0; whoever prefers books of their own writes tables and lengths and leaves the calls on pages alone.
+ * A page that only some sequences have filled is held by one of them: full pages may be shared.  Calls that read or write one cache go on one
+ * stream, or are put in order by the caller; calls that only read it (mt_attend) may overlap.
+ * Values are held feature by feature, a page's tokens side by side: that is how the products over tokens read them.
+ * In MT_KV8 a token's head_dim elements of one head share a scale, the least power of two (2^-126 at least) at which none exceeds 448; 1 where all
+ * are zero; infinite or NaN elements make scale and values of that token and head NaN. */
+#define MT_KV_MAX_SEQS 16384     /* most sequences of a cache                     */
+#define MT_KV_MAX_WIDTH 131072   /* most pages of a sequence                      */
+#define MT_KV_MAX_DIM 256        /* largest head_dim                              */
+#define MT_SAMPLE_MAX_CLASSES (1u << 20)
+typedef struct {
+    void* k;                    /* [layers][n_pages][heads][page_tokens][head_dim]; of page_stride, layer_stride elements  */
+    void* v;                    /* [layers][n_pages][heads][head_dim][page_tokens]; the same strides                       */
+    uint8_t* k_scales;          /* [layers][n_pages][heads][page_tokens], with MT_KV8, else NULL; of scales_..._stride bytes */
+    uint8_t* v_scales;          /* the same                                                                                */
+    int32_t* table;             /* [seqs][table_stride]                                                                    */
+    int32_t* lengths;           /* [seqs]                                                                                  */
+    int32_t* refs;              /* [n_pages]; calls on pages only                                                          */
+    void* work;                 /* work_bytes of mt_kv_work_get's size, 16-byte boundary; calls on pages only              */
+    uint64_t page_stride, layer_stride, scales_page_stride, scales_layer_stride, table_stride, work_bytes;
+    uint32_t dtype;             /* MT_F32, MT_BF16 or MT_KV8                                                               */
+    uint32_t layers, n_pages, heads;
+    uint32_t page_tokens;       /* 16, 32, 64, 128 or 256                                                                  */
+    uint32_t head_dim;          /* a multiple of 16 up to MT_KV_MAX_DIM                                                    */
+    uint32_t seqs, table_width;
+} mt_kv_cache;
+/* Errors of a cache in every call: MT_EINVAL (null k, v, table or lengths, scales with other types than MT_KV8 or missing with it, sizes of 0, pages,
+ * strides or scales that are not on 16 bytes, strides that make pages or layers overlap, table_stride below table_width), MT_EUNSUPPORTED (dtype,
+ * page_tokens, head_dim, more than MT_KV_MAX_SEQS or MT_KV_MAX_WIDTH, 2^31 pages or more). */
+
+/* The rows of a call and whose they are: rows first_row[b] .. first_row[b + 1] - 1 are the last tokens, in their order, of sequence seqs[b], whose length
+ * counts them already.  seqs NULL: sequence b.  first_row NULL: row b (rows = n_seqs).  Rows in no sequence are left as they are; a row that first_row would put outside 0 .. rows is
+ * none.  max_new: the most rows of a sequence, which the work is cut by; more are served too, but slowly.  No row stands in two sequences. */
+typedef struct {
+    const int32_t* seqs;        /* [n_seqs], or NULL          */
+    const int32_t* first_row;   /* [n_seqs + 1], or NULL      */
+    uint32_t rows, n_seqs, max_new;
+    uint32_t reserved;
+} mt_kv_batch;
+
+/* Keys and values of the batch's rows into the pages of one layer: [heads][head_dim] elements a row, rounded once.  A row without a place (its sequence's
+ * number out of range, its token beyond the table's width, its page's number out of range, more rows than tokens) is not written.
+ * Errors: MT_EINVAL (null, a stride below heads x head_dim, layer out of range, rows other than n_seqs without first_row, max_new 0), MT_EUNSUPPORTED (rows neither MT_F32 nor MT_BF16, or
+ * of another type than a cache that is not MT_KV8), MT_ESTATE (host-only context), MT_EDEVICE. */
+typedef struct {
+    const void* k;              /* [rows][k_stride], dtype    */
+    const void* v;              /* [rows][v_stride], dtype    */
+    uint64_t k_stride, v_stride;
+    uint32_t dtype, layer;
+} mt_kv_write_args;
+mt_status mt_kv_write(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const mt_kv_batch* batch, const mt_kv_write_args* args);
+
+/* out = sum_t p_t v_t with p = softmax(scale * q.k_t) over the tokens t that a row sees, head by head: those up to itself, of these the last `window` (0: all).
+ * q_heads is a multiple of the cache's heads; query heads h * q_heads / heads and on share head h of the cache.  lse = log sum_t e^(scale q.k_t), with
+ * which results over several caches can be joined.  Products are exact for MT_BF16 and fp32 for MT_F32; sums and statistics are fp32; weights are rounded to bf16 where rows
+ * are MT_BF16; out is rounded once.
+ * A row that sees nothing (no tokens, its sequence's number out of range, or all its products -infinity) gets out 0 and lse -infinity.  Tokens in pages whose
+ * number is out of range, or beyond the table's width, are not seen.  What stands in tokens that are not seen does not matter.
+ * max_length: tokens of the longest sequence, which the work is cut by (0: the table's width); longer ones are served too, but slowly.
+ * scratch: as in mt_score, of mt_attend_scratch_get's size for the call's sizes.
+ * Errors: MT_EINVAL (null, q_heads no multiple of heads or 0, strides below q_heads x head_dim, layer out of range, scale not finite, scratch too small),
+ * MT_EUNSUPPORTED (types as in mt_kv_write, more than 65535 query heads), MT_ESTATE, MT_EDEVICE. */
+typedef struct {
+    const void* q;              /* [rows][q_stride], dtype           */
+    void* out;                  /* [rows][out_stride], dtype; may be q itself (same stride)  */
+    float* lse;                 /* [rows][q_heads], or NULL          */
+    void* scratch;
+    uint64_t scratch_bytes;
+    uint64_t q_stride, out_stride;
+    uint32_t q_heads, dtype, layer, window, max_length;
+    float scale;
+} mt_attend_args;
+mt_status mt_attend(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const mt_kv_batch* batch, const mt_attend_args* args);
+mt_status mt_attend_scratch_get(const mt_kv_cache* cache, const mt_kv_batch* batch, uint32_t q_heads, uint32_t max_length, uint64_t* bytes);
+
+/* Calls on pages.  Lists are DEVICE int32 [n], n at most the cache's seqs.  An entry that names no sequence (out of range) does nothing, nor does one whose
+ * sequence an earlier entry of the call has named (of mt_kv_fork: as a child).  granted[i] (or NULL): 1 where entry i was served, 0 where not.
+ *
+ * mt_kv_grow: room for tokens[i] more tokens of sequence seqs[i] (NULL: i); its length counts them from now on.  Entries take pages in the order of the list, free pages in the order
+ *   of their numbers.  An entry that would need more than table_width pages, or whose tokens are negative, takes none; one for whose pages, with all
+ *   before it, there are not enough free ones changes nothing; what needs no page is always served.
+ * mt_kv_fork: sequence children[i], which has no tokens, becomes a copy of sequence parents[i] as it was before the call: full pages are shared, a last page that is not full is copied into
+ *   a free one (all layers), taken as in mt_kv_grow.
+ * mt_kv_free: the sequences' pages are let go (table entries -1), their lengths are 0.
+ * mt_kv_compact: with n pages held, these are pages 0 .. n - 1 afterwards: the i-th held one from number n on moves into the i-th free one below (all layers), and the
+ *   tables follow.  *live (DEVICE, or NULL) receives n.
+ * mt_kv_copy: page from[i] is copied over page to[i] (all layers); tables and counts stay.  A pair out of range, or whose target an entry behind it names again, does nothing; a
+ *   page that stands in both lists may be copied before or after it is overwritten.  n may be any number.
+ * Errors: MT_EINVAL (null list, refs or work, work too small, n over seqs), MT_ESTATE, MT_EDEVICE. */
+mt_status mt_kv_grow(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const int32_t* seqs, const int32_t* tokens, uint32_t n, int32_t* granted);
+mt_status mt_kv_fork(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const int32_t* parents, const int32_t* children, uint32_t n, int32_t* granted);
+mt_status mt_kv_free(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const int32_t* seqs, uint32_t n);
+mt_status mt_kv_compact(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, int32_t* live);
+mt_status mt_kv_copy(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const int32_t* from, const int32_t* to, uint32_t n);
+mt_status mt_kv_work_get(uint32_t n_pages, uint32_t seqs, uint64_t* bytes);
+
+/* One class for every row of logits, drawn with the row's own settings (DEVICE fp32 or int32 [rows]; NULL: the setting that changes nothing).  Allowed classes and
+ * their order (falling logits, lower numbers first among equals) are mt_score's; w = e^((x - max) / temperature).  A row keeps
+ *   of its allowed classes the first top_k (0 or less: all), of these those with w >= min_p (0 or less: all; more than 1 counts as 1), of these the shortest front part that has top_p of their
+ *   weight (1 or more: all; the first always).
+ * Drawn is the first kept class, in the order of class numbers, up to which the kept classes have more than uniform[i] of their weight (uniform in [0, 1): a class is drawn with
+ * its share of the weight); with uniform of 1 or more the last one of any weight.  temperature 0 (or below 2^-126) keeps the first class alone.
+ * Weights are multiples of 2^-(62 - ceil(log2 classes)), from 64-bit exponentials; sums of them are exact, so results depend on nothing but the inputs.
+ *   ids[i]: the class; logprobs[i] = log of its share of the kept weight; kept[i]: classes kept.  Each may be NULL, not all.
+ * A row without an allowed class: -1, -infinity, 0.  A row with a NaN or +infinity among its allowed classes or a setting that is NaN, or with a negative temperature: -1, NaN, -1.
+ * scratch: as in mt_score, of mt_sample_scratch_get's size.
+ * Errors: as mt_score; MT_EUNSUPPORTED for more than MT_SAMPLE_MAX_CLASSES classes too. */
+typedef struct {
+    const void* logits;             /* [rows][row_stride], dtype                */
+    const int32_t* n_classes;       /* [rows], or NULL; taken into 0 .. classes */
+    const uint32_t* allowed;        /* [rows][allowed_stride], or NULL          */
+    const float* uniform;           /* [rows]                                   */
+    const float* temperature;       /* [rows], or NULL: 1                       */
+    const int32_t* top_k;           /* [rows], or NULL: all                     */
+    const float* top_p;             /* [rows], or NULL: 1                       */
+    const float* min_p;             /* [rows], or NULL: 0                       */
+    int32_t* ids;                   /* [rows], or NULL                          */
+    float* logprobs;                /* [rows], or NULL                          */
+    int32_t* kept;                  /* [rows], or NULL                          */
+    void* scratch;
+    uint64_t scratch_bytes;
+    uint64_t row_stride, allowed_stride;
+    uint32_t rows, classes, dtype;
+    uint32_t reserved;
+} mt_sample_args;
+mt_status mt_sample(mt_ctx* ctx, void* hip_stream, const mt_sample_args* args);
+mt_status mt_sample_scratch_get(uint32_t rows, uint32_t classes, uint64_t* bytes);
 
 /* Text of the last error on this context ("" if none); valid until the next call. */
 const char* mt_last_error(const mt_ctx* ctx);

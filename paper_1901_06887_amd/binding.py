@@ -21,10 +21,11 @@ STATUS_NAMES = {0: "MT_OK", 1: "MT_EINVAL", 2: "MT_ENOMEM", 3: "MT_ENOTFOUND", 4
                 5: "MT_EUNSUPPORTED", 6: "MT_EFULL", 7: "MT_ESTATE", 8: "MT_EDEVICE"}
 MT_FC, MT_CONV2D, MT_GAP, MT_MAXPOOL, MT_ADD = 0, 1, 2, 3, 4
 MT_ACT_NONE, MT_ACT_RELU, MT_ACT_GELU = 0, 1, 2
-MT_F32, MT_BF16, MT_MX8 = 0, 1, 2
+MT_F32, MT_BF16, MT_MX8, MT_KV8 = 0, 1, 2, 3
 MT_MAX_LAYERS = 48
 MT_MX_BLOCK = 32
 MT_SCORE_MAX_TOP, MT_SCORE_MAX_GIVEN = 32, 16
+MT_KV_MAX_SEQS, MT_KV_MAX_WIDTH, MT_KV_MAX_DIM, MT_SAMPLE_MAX_CLASSES = 16384, 131072, 256, 1 << 20
 
 
 class MtError(RuntimeError):
@@ -99,6 +100,30 @@ class mt_score_args(ctypes.Structure):
                 [(n, ctypes.c_uint32) for n in ("rows", "classes", "n_given", "top", "dtype")] + [("temperature", ctypes.c_float)])
 
 
+class mt_kv_cache(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales", "table", "lengths", "refs", "work")] +
+                [(n, ctypes.c_uint64) for n in ("page_stride", "layer_stride", "scales_page_stride", "scales_layer_stride", "table_stride", "work_bytes")] +
+                [(n, ctypes.c_uint32) for n in ("dtype", "layers", "n_pages", "heads", "page_tokens", "head_dim", "seqs", "table_width")])
+
+
+class mt_kv_batch(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("seqs", "first_row")] + [(n, ctypes.c_uint32) for n in ("rows", "n_seqs", "max_new", "reserved")]
+
+
+class mt_kv_write_args(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v")] + [(n, ctypes.c_uint64) for n in ("k_stride", "v_stride")] + [(n, ctypes.c_uint32) for n in ("dtype", "layer")]
+
+
+class mt_attend_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("q", "out", "lse", "scratch")] + [(n, ctypes.c_uint64) for n in ("scratch_bytes", "q_stride", "out_stride")] +
+                [(n, ctypes.c_uint32) for n in ("q_heads", "dtype", "layer", "window", "max_length")] + [("scale", ctypes.c_float)])
+
+
+class mt_sample_args(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("logits", "n_classes", "allowed", "uniform", "temperature", "top_k", "top_p", "min_p", "ids", "logprobs", "kept", "scratch")] +
+                [(n, ctypes.c_uint64) for n in ("scratch_bytes", "row_stride", "allowed_stride")] + [(n, ctypes.c_uint32) for n in ("rows", "classes", "dtype", "reserved")])
+
+
 class mt_profile(ctypes.Structure):
     _fields_ = [("batcher_ms", ctypes.c_float), ("gather_ms", ctypes.c_float), ("head_ms", ctypes.c_float),
                 ("fc_ms", ctypes.c_float * MT_MAX_LAYERS), ("fc_big_ms", ctypes.c_float * MT_MAX_LAYERS), ("conv_ms", ctypes.c_float * MT_MAX_LAYERS),
@@ -159,6 +184,16 @@ def load_library() -> ctypes.CDLL:
     L.mt_score.argtypes = [vp, vp, ctypes.POINTER(mt_score_args)]
     L.mt_debug_linear4_shape.argtypes = [ctypes.c_uint64, u32, u32, u32, u32, ctypes.POINTER(u32), ctypes.POINTER(u32)]
     L.mt_score_scratch_get.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_uint64)]
+    cache, batch, u64p = ctypes.POINTER(mt_kv_cache), ctypes.POINTER(mt_kv_batch), ctypes.POINTER(ctypes.c_uint64)
+    L.mt_kv_write.argtypes = [vp, vp, cache, batch, ctypes.POINTER(mt_kv_write_args)]
+    L.mt_attend.argtypes = [vp, vp, cache, batch, ctypes.POINTER(mt_attend_args)]
+    L.mt_attend_scratch_get.argtypes = [cache, batch, u32, u32, u64p]
+    L.mt_kv_grow.argtypes = L.mt_kv_fork.argtypes = [vp, vp, cache, vp, vp, u32, vp]
+    L.mt_kv_free.argtypes = [vp, vp, cache, vp, u32]
+    L.mt_kv_compact.argtypes = [vp, vp, cache, vp]
+    L.mt_kv_copy.argtypes = [vp, vp, cache, vp, vp, u32]
+    L.mt_kv_work_get.argtypes = L.mt_sample_scratch_get.argtypes = [u32, u32, u64p]
+    L.mt_sample.argtypes = [vp, vp, ctypes.POINTER(mt_sample_args)]
     L.mt_last_error.argtypes = [vp]
     L.mt_last_error.restype = ctypes.c_char_p
     L.mt_version.restype = ctypes.c_char_p
@@ -166,7 +201,8 @@ def load_library() -> ctypes.CDLL:
                  "mt_submit_batch", "mt_run", "mt_run_static", "mt_last_counts", "mt_get_stats", "mt_tenant_account_get", "mt_estimate_run", "mt_prefetch", "mt_cache_stats_get", "mt_admit", "mt_debug_poison", "mt_debug_copy",
                  "mt_set_profiling", "mt_get_profile", "mt_model_footprint_get", "mt_debug_mfma_rate",
                  "mt_debug_conv_launch", "mt_add_norm", "mt_register_matrix4", "mt_matrix4_footprint_get", "mt_unregister_matrix4", "mt_linear4", "mt_linear4_within",
-                 "mt_score", "mt_score_scratch_get", "mt_debug_linear4_shape"):
+                 "mt_score", "mt_score_scratch_get", "mt_debug_linear4_shape", "mt_kv_write", "mt_attend", "mt_attend_scratch_get", "mt_kv_grow", "mt_kv_fork", "mt_kv_free",
+                 "mt_kv_compact", "mt_kv_copy", "mt_kv_work_get", "mt_sample", "mt_sample_scratch_get"):
         getattr(L, name).restype = ctypes.c_int
     _lib = L
     return L
@@ -360,6 +396,31 @@ class Context:
         st = self._lib.mt_score(self._h, stream_ptr, ctypes.byref(args))
         self._check(st)
 
+    # -- caches of language models (struct arguments as in mt.h; lists are device pointers) -------
+    def kv_write(self, stream_ptr: int, cache, batch, args):
+        self._check(self._lib.mt_kv_write(self._h, stream_ptr, ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(args)))
+
+    def attend(self, stream_ptr: int, cache, batch, args):
+        self._check(self._lib.mt_attend(self._h, stream_ptr, ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(args)))
+
+    def kv_grow(self, stream_ptr: int, cache, seqs, tokens, n: int, granted=None):
+        self._check(self._lib.mt_kv_grow(self._h, stream_ptr, ctypes.byref(cache), seqs, tokens, n, granted))
+
+    def kv_fork(self, stream_ptr: int, cache, parents, children, n: int, granted=None):
+        self._check(self._lib.mt_kv_fork(self._h, stream_ptr, ctypes.byref(cache), parents, children, n, granted))
+
+    def kv_free(self, stream_ptr: int, cache, seqs, n: int):
+        self._check(self._lib.mt_kv_free(self._h, stream_ptr, ctypes.byref(cache), seqs, n))
+
+    def kv_compact(self, stream_ptr: int, cache, live=None):
+        self._check(self._lib.mt_kv_compact(self._h, stream_ptr, ctypes.byref(cache), live))
+
+    def kv_copy(self, stream_ptr: int, cache, from_pages, to_pages, n: int):
+        self._check(self._lib.mt_kv_copy(self._h, stream_ptr, ctypes.byref(cache), from_pages, to_pages, n))
+
+    def sample(self, stream_ptr: int, args):
+        self._check(self._lib.mt_sample(self._h, stream_ptr, ctypes.byref(args)))
+
     def stats(self) -> dict:
         s = mt_stats()
         self._check(self._lib.mt_get_stats(self._h, ctypes.byref(s)))
@@ -397,6 +458,33 @@ def score_scratch(rows: int, classes: int, n_given: int, top: int) -> int:
     st = load_library().mt_score_scratch_get(rows, classes, n_given, top, ctypes.byref(n))
     if st != MT_OK:
         raise MtError(st, "%d classes, %d given, %d alternatives" % (classes, n_given, top))
+    return int(n.value)
+
+
+def kv_work(n_pages: int, seqs: int) -> int:
+    """mt_kv_work_get: bytes of work memory of a cache of these sizes."""
+    n = ctypes.c_uint64()
+    st = load_library().mt_kv_work_get(n_pages, seqs, ctypes.byref(n))
+    if st != MT_OK:
+        raise MtError(st, "no cache has %d pages and %d sequences" % (n_pages, seqs))
+    return int(n.value)
+
+
+def attend_scratch(cache: mt_kv_cache, n_seqs: int, q_heads: int, max_new: int = 1, max_length: int = 0) -> int:
+    """mt_attend_scratch_get: bytes of scratch that a call of these sizes needs."""
+    n = ctypes.c_uint64()
+    st = load_library().mt_attend_scratch_get(ctypes.byref(cache), ctypes.byref(mt_kv_batch(None, None, n_seqs, n_seqs, max_new, 0)), q_heads, max_length, ctypes.byref(n))
+    if st != MT_OK:
+        raise MtError(st, "%d query heads on %d heads of %d, %d sequences" % (q_heads, cache.heads, cache.head_dim, n_seqs))
+    return int(n.value)
+
+
+def sample_scratch(rows: int, classes: int) -> int:
+    """mt_sample_scratch_get: bytes of scratch that a call of these sizes needs."""
+    n = ctypes.c_uint64()
+    st = load_library().mt_sample_scratch_get(rows, classes, ctypes.byref(n))
+    if st != MT_OK:
+        raise MtError(st, "%d classes" % classes)
     return int(n.value)
 
 

@@ -9,7 +9,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmt.so")
 CALLS = os.path.join(HERE, "_answers.so")
 SOURCES = ["mt_api.cpp", "batcher.hip", "fc_stream.hip", "fc_big.hip", "conv.hip", "conv_first.hip", "small.hip",
-           "lm_api.cpp", "lm_norm.hip", "lm_linear4.hip", "lm_score.hip"]
+           "lm_api.cpp", "lm_norm.hip", "lm_linear4.hip", "lm_score.hip",
+           "lm_cache_api.cpp", "lm_kv_write.hip", "lm_attend.hip", "lm_pages.hip", "lm_sample.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm",
          # keep the compiler from forming packed-fp32 VALU ops
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

@@ -12,7 +12,7 @@
 #include <string>
 #include <vector>
 
-#include "lm_internal.h"
+#include "lm_cache.h"
 #include "../../include/mt_debug.h"
 
 using namespace mt;
@@ -1411,6 +1411,7 @@ mt_status mt_create(mt_ctx** out, const mt_config* cfg)
     CREATE_TRY(prepare_conv(cfg->dtype));
     CREATE_TRY(prepare_conv_first(cfg->dtype));
     CREATE_TRY(prepare_linear4());
+    CREATE_TRY(prepare_pages());
     const uint64_t R = cfg->max_requests, T = cfg->max_tenants;
     CREATE_TRY(hipMalloc((void**)&c->d_arena, c->cfg.arena_bytes));
     CREATE_TRY(hipMalloc((void**)&c->d_tenants, T * sizeof(TenantDev)));

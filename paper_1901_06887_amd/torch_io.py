@@ -90,7 +90,8 @@ def answers():
             from . import _answers as calls
         except ImportError as e:
             raise ImportError("_answers.so is missing or was built for another torch: build it with `python -m paper_1901_06887_amd.build` (%s)" % e)
-        calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.mt_add_norm, lib.mt_linear4_within, lib.mt_score)))
+        calls.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.mt_add_norm, lib.mt_linear4_within, lib.mt_score, lib.mt_kv_write, lib.mt_attend, lib.mt_kv_grow, lib.mt_kv_fork,
+                                                                           lib.mt_kv_free, lib.mt_kv_compact, lib.mt_kv_copy, lib.mt_sample)))
         _answers = calls
     return _answers
 
@@ -141,6 +142,127 @@ def score(ctx: B.Context, logits: torch.Tensor, out: Scores, given: Optional[tor
     the best alternatives.  n_classes: int32 [rows]; allowed: int32 [rows, words], a bit for every class.  Forward only."""
     st = (_answers or answers()).score(ctx._h.value or 0, stream.cuda_stream if stream is not None else _raw_stream(ctx.device), ctx.device, logits, given, n_classes, allowed,
                                        temperature, out.given_logprobs, out.given_ranks, out.entropy, out.top_ids, out.top_logprobs, out.scratch)
+    if st:
+        ctx._check(st)
+    return out
+
+
+# ---- caches of language models -----------------------------------------------------------------------
+_KV_TYPES = {B.MT_F32: torch.float32, B.MT_BF16: torch.bfloat16, B.MT_KV8: torch.float8_e4m3fn}
+
+
+class KVCache:
+    """A paged cache (mt_kv_cache): its tensors, and their description as the calls take it.
+
+    k [layers, pages, heads, page_tokens, head_dim], v [layers, pages, heads, head_dim, page_tokens]; with MT_KV8 k_scales, v_scales float8_e8m0fnu
+    [layers, pages, heads, page_tokens]; table int32 [seqs, width], lengths int32 [seqs], refs int32 [pages], work uint8."""
+
+    def __init__(self, k, v, k_scales, v_scales, table, lengths, refs, work, dtype: int):
+        self.k, self.v, self.k_scales, self.v_scales, self.table, self.lengths, self.refs, self.work = k, v, k_scales, v_scales, table, lengths, refs, work
+        layers, pages, heads, page_tokens, head_dim = k.shape
+        p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.spec = B.mt_kv_cache(p(k), p(v), p(k_scales), p(v_scales), p(table), p(lengths), p(refs), p(work), k.stride(1), k.stride(0),
+                                  0 if k_scales is None else k_scales.stride(1), 0 if k_scales is None else k_scales.stride(0), table.stride(0), work.numel(),
+                                  dtype, layers, pages, heads, page_tokens, head_dim, table.shape[0], table.shape[1])
+        self._tensors = (k, v, k_scales, v_scales, table, lengths, refs)      # (the spec has their addresses)
+
+
+def alloc_kv(pages: int, page_tokens: int, heads: int, head_dim: int, seqs: int, width: int, dtype: int = B.MT_BF16, layers: int = 1, device="cuda:0") -> KVCache:
+    """An empty cache of so many pages, for `seqs` sequences of up to `width` pages each.  dtype: MT_F32, MT_BF16 or MT_KV8."""
+    if dtype not in _KV_TYPES:
+        raise ValueError("a cache of dtype %r" % (dtype,))
+    buf = lambda t, *shape: torch.empty(shape, dtype=t, device=device)  # noqa: E731
+    scales = (lambda: buf(torch.uint8, layers, pages, heads, page_tokens).fill_(127).view(torch.float8_e8m0fnu)) if dtype == B.MT_KV8 else lambda: None
+    return KVCache(buf(_KV_TYPES[dtype], layers, pages, heads, page_tokens, head_dim), buf(_KV_TYPES[dtype], layers, pages, heads, head_dim, page_tokens), scales(), scales(),
+                   buf(torch.int32, seqs, width).fill_(-1), buf(torch.int32, seqs).zero_(), buf(torch.int32, pages).zero_(), buf(torch.uint8, B.kv_work(pages, seqs)), dtype)
+
+
+def _where(ctx: B.Context, stream):
+    return ctx._h.value or 0, stream.cuda_stream if stream is not None else _raw_stream(ctx.device), ctx.device
+
+
+def kv_write(ctx: B.Context, cache: KVCache, k: torch.Tensor, v: torch.Tensor, seqs: Optional[torch.Tensor] = None, first_row: Optional[torch.Tensor] = None, max_new: int = 1,
+             layer: int = 0, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_kv_write on the given (or current) stream: keys and values [rows, heads * head_dim] of the last tokens of every sequence into their pages.  seqs: int32, the
+    sequences of the batch (None: 0, 1, ...); first_row: int32, one more than there are (None: a row each); max_new: most rows of a sequence."""
+    st = (_answers or answers()).kv_write(*_where(ctx, stream), cache.spec, cache._tensors, k, v, seqs, first_row, max_new, layer)
+    if st:
+        ctx._check(st)
+
+
+def alloc_attend(ctx: B.Context, cache: KVCache, q_heads: int, n_seqs: int, max_new: int = 1, max_length: int = 0) -> torch.Tensor:
+    """Scratch of mt_attend for batches of so many sequences.  One call at a time may use it."""
+    return torch.zeros(B.attend_scratch(cache.spec, n_seqs, q_heads, max_new, max_length), dtype=torch.uint8, device=cache.k.device)
+
+
+def attend(ctx: B.Context, cache: KVCache, q: torch.Tensor, out: torch.Tensor, seqs: Optional[torch.Tensor] = None, first_row: Optional[torch.Tensor] = None, max_new: int = 1,
+           max_length: int = 0, window: int = 0, scale: Optional[float] = None, lse: Optional[torch.Tensor] = None, layer: int = 0, scratch: Optional[torch.Tensor] = None,
+           stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_attend on the given (or current) stream: rows q [rows, q_heads * head_dim] of the last tokens of every sequence (whose keys and values are written already)
+    attend to all of it, each up to itself; out like q, lse float32 [rows, q_heads].  seqs, first_row, max_new: as in kv_write.  max_length: tokens of the longest sequence
+    (0: what the table holds).  window: tokens that a row sees (0: all).  scale: None for head_dim^-0.5.  scratch: alloc_attend's for the same sizes.  Forward only."""
+    st = (_answers or answers()).attend(*_where(ctx, stream), cache.spec, cache._tensors, q, out, seqs, first_row, max_new, layer, window, max_length, scale, lse, scratch)
+    if st:
+        ctx._check(st)
+
+
+def kv_grow(ctx: B.Context, cache: KVCache, tokens: torch.Tensor, seqs: Optional[torch.Tensor] = None, granted: Optional[torch.Tensor] = None,
+            stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_kv_grow: room for tokens[i] (int32) more tokens of sequence seqs[i] (None: i); granted[i] says whether there was."""
+    st = (_answers or answers()).kv_grow(*_where(ctx, stream), cache.spec, cache._tensors, seqs, tokens, granted)
+    if st:
+        ctx._check(st)
+
+
+def kv_fork(ctx: B.Context, cache: KVCache, parents: torch.Tensor, children: torch.Tensor, granted: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_kv_fork: the empty sequence children[i] becomes a copy of parents[i] that shares its full pages."""
+    st = (_answers or answers()).kv_fork(*_where(ctx, stream), cache.spec, cache._tensors, parents, children, granted)
+    if st:
+        ctx._check(st)
+
+
+def kv_free(ctx: B.Context, cache: KVCache, seqs: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_kv_free: the sequences let go of their pages."""
+    st = (_answers or answers()).kv_free(*_where(ctx, stream), cache.spec, cache._tensors, seqs)
+    if st:
+        ctx._check(st)
+
+
+def kv_compact(ctx: B.Context, cache: KVCache, live: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_kv_compact: held pages move to the lowest numbers; live (int32 [1]) receives how many there are."""
+    st = (_answers or answers()).kv_compact(*_where(ctx, stream), cache.spec, cache._tensors, live)
+    if st:
+        ctx._check(st)
+
+
+def kv_copy(ctx: B.Context, cache: KVCache, from_pages: torch.Tensor, to_pages: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """mt_kv_copy: pages of all layers copied over others."""
+    st = (_answers or answers()).kv_copy(*_where(ctx, stream), cache.spec, cache._tensors, from_pages, to_pages)
+    if st:
+        ctx._check(st)
+
+
+@dataclass
+class Samples:
+    """Outputs of mt_sample; one that is set to None is left out."""
+    ids: Optional[torch.Tensor]              # int32 [R]
+    logprobs: Optional[torch.Tensor]         # float32 [R]
+    kept: Optional[torch.Tensor]             # int32 [R]
+    scratch: torch.Tensor                    # uint8
+
+
+def alloc_samples(rows: int, classes: int, device="cuda:0") -> Samples:
+    """Outputs and scratch of mt_sample for so many rows and classes.  One call at a time may use them."""
+    ints = lambda: torch.empty(rows, dtype=torch.int32, device=device)  # noqa: E731
+    return Samples(ints(), torch.empty(rows, dtype=torch.float32, device=device), ints(), torch.zeros(B.sample_scratch(rows, classes), dtype=torch.uint8, device=device))
+
+
+def sample(ctx: B.Context, logits: torch.Tensor, uniform: torch.Tensor, out: Samples, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+           top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None, n_classes: Optional[torch.Tensor] = None, allowed: Optional[torch.Tensor] = None,
+           stream: Optional[torch.cuda.Stream] = None) -> Samples:
+    """mt_sample on the given (or current) stream: one class for every row of logits, from the random numbers uniform (float32 [rows], in [0, 1)) and the rows' settings: temperature,
+    top_p, min_p float32 [rows], top_k int32 [rows].  n_classes, allowed: as in score.  Forward only."""
+    st = (_answers or answers()).sample(*_where(ctx, stream), logits, uniform, temperature, top_k, top_p, min_p, n_classes, allowed, out.ids, out.logprobs, out.kept, out.scratch)
     if st:
         ctx._check(st)
     return out
