@@ -530,7 +530,7 @@ mt_status mt_kv_write(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, c
  * max_length: tokens of the longest sequence, which the work is cut by (0: the table's width); longer ones are served too, but slowly.
  * scratch: as in mt_score, of mt_attend_scratch_get's size for the call's sizes.
  * Errors: MT_EINVAL (null, q_heads no multiple of heads or 0, strides below q_heads x head_dim, layer out of range, scale not finite, scratch too small),
- * MT_EUNSUPPORTED (types as in mt_kv_write, more than 65535 query heads), MT_ESTATE, MT_EDEVICE. */
+ * MT_EUNSUPPORTED (types as in mt_kv_write, more than 65535 query heads, 2^20 sequences in a batch or 2^23 pairs of these and heads), MT_ESTATE, MT_EDEVICE. */
 typedef struct {
     const void* q;              /* [rows][q_stride], dtype           */
     void* out;                  /* [rows][out_stride], dtype; may be q itself (same stride)  */

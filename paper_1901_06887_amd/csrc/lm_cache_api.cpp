@@ -8,6 +8,7 @@ using namespace mt;
 namespace {
 
 constexpr uint32_t kMaxEntries = 1u << 20;       // of a batch
+constexpr uint32_t kMaxPairs = 1u << 23;         // of a batch's sequences and heads
 constexpr uint32_t kMaxQueryHeads = 65535;       // (a grid's second dimension)
 
 #define LM_TRY(c, expr)                                                                                                     \
@@ -62,7 +63,7 @@ mt_status check_batch(mt_ctx* c, const mt_kv_cache* k, const mt_kv_batch* b, uin
     if (!b->first_row && b->rows != b->n_seqs) return ctx_fail(c, MT_EINVAL, "%u rows of %u sequences, but no first_row", b->rows, b->n_seqs);
     if (!b->seqs && b->n_seqs > k->seqs) return ctx_fail(c, MT_EINVAL, "%u sequences of a cache of %u", b->n_seqs, k->seqs);
     if (b->rows && b->max_new == 0) return ctx_fail(c, MT_EINVAL, "max_new is 0");
-    if (b->n_seqs > kMaxEntries) return ctx_fail(c, MT_EUNSUPPORTED, "%u sequences in a batch", b->n_seqs);
+    if (b->n_seqs > kMaxEntries || (uint64_t)b->n_seqs * k->heads > kMaxPairs) return ctx_fail(c, MT_EUNSUPPORTED, "%u sequences in a batch", b->n_seqs);
     if (b->rows > (uint32_t)INT32_MAX) return ctx_fail(c, MT_EUNSUPPORTED, "%u rows", b->rows);
     return MT_OK;
 }
@@ -112,9 +113,9 @@ mt_status mt_kv_write(mt_ctx* c, void* hip_stream, const mt_kv_cache* k, const m
 
 mt_status mt_attend_scratch_get(const mt_kv_cache* k, const mt_kv_batch* b, uint32_t q_heads, uint32_t max_length, uint64_t* bytes)
 {
-    if (!k || !b || !bytes || !k->heads || !k->page_tokens || !k->table_width || q_heads == 0 || q_heads % k->heads || q_heads > kMaxQueryHeads || b->n_seqs > kMaxEntries) return MT_EINVAL;
+    if (!k || !b || !bytes || !k->heads || !k->page_tokens || !k->table_width || q_heads == 0 || q_heads % k->heads || q_heads > kMaxQueryHeads || b->n_seqs > kMaxEntries || (uint64_t)b->n_seqs * k->heads > kMaxPairs) return MT_EINVAL;
     if (k->head_dim == 0 || k->head_dim > MT_KV_MAX_DIM || k->head_dim % 16) return MT_EUNSUPPORTED;
-    *bytes = attend_scratch_bytes(*k, *b, q_heads, max_length);
+    *bytes = b->n_seqs ? attend_scratch_bytes(*k, *b, q_heads, max_length) : 0;
     return MT_OK;
 }
 
@@ -126,7 +127,7 @@ mt_status mt_attend(mt_ctx* c, void* hip_stream, const mt_kv_cache* k, const mt_
     if (st == MT_OK) st = check_batch(c, k, b, a->dtype, a->layer);
     if (st != MT_OK) return st;
     if (a->q_heads == 0 || a->q_heads % k->heads) return ctx_fail(c, MT_EINVAL, "%u query heads on %u heads", a->q_heads, k->heads);
-    if (a->q_heads > kMaxQueryHeads) return ctx_fail(c, MT_EUNSUPPORTED, "%u query heads", a->q_heads);
+    if (a->q_heads > kMaxQueryHeads || (uint64_t)b->rows * (a->q_heads / k->heads) > (uint32_t)INT32_MAX) return ctx_fail(c, MT_EUNSUPPORTED, "%u rows of %u query heads", b->rows, a->q_heads);
     const uint64_t width = (uint64_t)a->q_heads * k->head_dim;
     if (b->rows && (!a->q || !a->out)) return ctx_fail(c, MT_EINVAL, "null rows");
     if (a->q_stride < width || a->out_stride < width) return ctx_fail(c, MT_EINVAL, "a stride is below the %llu elements of a row", (unsigned long long)width);

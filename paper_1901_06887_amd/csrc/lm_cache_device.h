@@ -7,30 +7,31 @@ namespace mt {
 
 inline uint32_t value_bytes(uint32_t dtype) { return dtype == MT_F32 ? 4 : dtype == MT_BF16 ? 2 : 1; }
 
-// Batch entry b: its sequence, and rows first .. last - 1 of the call's; row r is token length - (after - r).
+// Batch entry b: its sequence, and rows first .. last - 1 of the call's; row r is token length - (after - r).  (Rows are below 2^31, so nothing here leaves 32 bits.)
 struct SeqRows {
     int32_t seq;                 // -1: none
-    int32_t length;
-    int64_t first, last, after;
+    int32_t length, first, last, after;
+    // tokens up to row `first + j` and with it; 0 or less: it stands in front of the sequence
+    __device__ __forceinline__ int32_t upto(int32_t j) const { return length - (after - (first + j)) + 1; }
 };
 __device__ __forceinline__ SeqRows seq_rows(const mt_kv_cache& c, const mt_kv_batch& b, uint32_t i)
 {
     SeqRows r;
     const int32_t seq = b.seqs ? b.seqs[i] : (int32_t)i;
-    const int64_t f0 = b.first_row ? b.first_row[i] : (int64_t)i, f1 = b.first_row ? b.first_row[i + 1] : (int64_t)i + 1;
+    const int32_t f0 = b.first_row ? b.first_row[i] : (int32_t)i;
+    r.after = b.first_row ? b.first_row[i + 1] : (int32_t)i + 1;
     const bool there = (uint32_t)seq < c.seqs;
     r.seq = there ? seq : -1;
     r.length = there ? max(c.lengths[seq], 0) : 0;
-    r.first = max(f0, (int64_t)0);
-    r.last = min(f1, (int64_t)b.rows);
-    r.after = f1;
+    r.first = max(f0, 0);
+    r.last = min(r.after, (int32_t)b.rows);
     return r;
 }
 
 // Page of a token of sequence `seq`; -1 where it has none.
-__device__ __forceinline__ int32_t page_of(const mt_kv_cache& c, int32_t seq, int64_t token)
+__device__ __forceinline__ int32_t page_of(const mt_kv_cache& c, int32_t seq, int32_t token)
 {
-    const uint64_t i = (uint64_t)token / c.page_tokens;
+    const uint32_t i = (uint32_t)token / c.page_tokens;
     if (token < 0 || i >= c.table_width) return -1;
     const int32_t p = c.table[(uint64_t)seq * c.table_stride + i];
     return (uint32_t)p < c.n_pages ? p : -1;

@@ -14,8 +14,9 @@ __global__ void __launch_bounds__(256) kv_write_kernel(KvWriteArgs w)
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = c.head_dim;
     const SeqRows s = seq_rows(c, w.b, blockIdx.x);
     if (s.seq < 0) return;
-    for (int64_t r = s.first + blockIdx.y; r < s.last; r += gridDim.y) {
-        const int64_t token = s.length - (s.after - r);
+    for (uint32_t j = blockIdx.y; (int32_t)j < s.last - s.first; j += gridDim.y) {
+        const int32_t token = s.upto((int32_t)j) - 1;
+        const int64_t r = s.first + (int32_t)j;
         const int32_t page = page_of(c, s.seq, token);
         if (page < 0) continue;
         const uint32_t slot = (uint32_t)token % c.page_tokens;
