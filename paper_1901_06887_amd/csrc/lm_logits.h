@@ -61,16 +61,17 @@ template <typename T, uint32_t VECS> struct Raw {
 #pragma unroll
             for (uint32_t i = 0; i < kVecs; ++i) {
                 const uint32_t c = first(base, i, lane);
-                v[i] = u32x4{0, 0, 0, 0};
-                if (c + kVec <= classes) v[i] = *(const typename Any<T>::vec16*)(x + c);
+                u32x4 w{0, 0, 0, 0};
+                if (c + kVec <= classes) w = *(const typename Any<T>::vec16*)(x + c);
                 else if (c < classes) {
 #pragma unroll
                     for (uint32_t e = 0; e < kVec; ++e)
                         if (c + e < classes) {
-                            if constexpr (sizeof(T) == 2) v[i][e / 2] |= (uint32_t)((const uint16_t*)x)[c + e] << (16 * (e % 2));
-                            else v[i][e] = ((const uint32_t*)x)[c + e];
+                            if constexpr (sizeof(T) == 2) w[e / 2] |= (uint32_t)((const uint16_t*)x)[c + e] << (16 * (e % 2));
+                            else w[e] = ((const uint32_t*)x)[c + e];
                         }
                 }
+                v[i] = w;
             }
         }
         if constexpr (MASK) {

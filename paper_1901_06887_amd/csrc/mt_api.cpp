@@ -1412,6 +1412,7 @@ mt_status mt_create(mt_ctx** out, const mt_config* cfg)
     CREATE_TRY(prepare_conv_first(cfg->dtype));
     CREATE_TRY(prepare_linear4());
     CREATE_TRY(prepare_pages());
+    CREATE_TRY(prepare_sample());
     const uint64_t R = cfg->max_requests, T = cfg->max_tenants;
     CREATE_TRY(hipMalloc((void**)&c->d_arena, c->cfg.arena_bytes));
     CREATE_TRY(hipMalloc((void**)&c->d_tenants, T * sizeof(TenantDev)));
