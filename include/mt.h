@@ -523,8 +523,8 @@ mt_status mt_kv_write(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, c
 
 /* out = sum_t p_t v_t with p = softmax(scale * q.k_t) over the tokens t that a row sees, head by head: those up to itself, of these the last `window` (0: all).
  * q_heads is a multiple of the cache's heads; query heads h * q_heads / heads and on share head h of the cache.  lse = log sum_t e^(scale q.k_t), with
- * which results over several caches can be joined.  Products are exact for MT_BF16 and fp32 for MT_F32; sums and statistics are fp32; weights are rounded to bf16 where rows
- * are MT_BF16; out is rounded once.
+ * which results over several caches can be joined.  Products are exact for MT_BF16 and fp32 for MT_F32; sums and statistics are fp32; where rows are MT_BF16 weights
+ * are off by 2^-17 of themselves on top; out is rounded once.
  * A row that sees nothing (no tokens, its sequence's number out of range, or all its products -infinity) gets out 0 and lse -infinity.  Tokens in pages whose
  * number is out of range, or beyond the table's width, are not seen.  What stands in tokens that are not seen does not matter.
  * max_length: tokens of the longest sequence, which the work is cut by (0: the table's width); longer ones are served too, but slowly.
@@ -571,7 +571,8 @@ mt_status mt_kv_work_get(uint32_t n_pages, uint32_t seqs, uint64_t* bytes);
  *   weight (1 or more: all; the first always).
  * Drawn is the first kept class, in the order of class numbers, up to which the kept classes have more than uniform[i] of their weight (uniform in [0, 1): a class is drawn with
  * its share of the weight); with uniform of 1 or more the last one of any weight.  temperature 0 (or below 2^-126) keeps the first class alone.
- * Weights are multiples of 2^-(62 - ceil(log2 classes)), from 64-bit exponentials; sums of them are exact, so results depend on nothing but the inputs.
+ * Weights are off by 2^-39 of themselves and summed in 64 bits, in an order that depends on nothing but the inputs: a class whose border lies nearer than that to where top_p or the random number falls may
+ * be taken for its neighbour.
  *   ids[i]: the class; logprobs[i] = log of its share of the kept weight; kept[i]: classes kept.  Each may be NULL, not all.
  * A row without an allowed class: -1, -infinity, 0.  A row with a NaN or +infinity among its allowed classes or a setting that is NaN, or with a negative temperature: -1, NaN, -1.
  * scratch: as in mt_score, of mt_sample_scratch_get's size.

@@ -113,9 +113,11 @@ template <typename T, typename C, int D, bool EXACT> struct Shape {
     // p: the weights as the second product takes them.
     static constexpr int kWeights = kWide ? kEach : kEach / 8;
     struct Weights {
-        u32x4 v[kWide ? 1 : kEach / 8];
+        u32x4 v[kWide ? 1 : kEach / 8], rest[kWide ? 1 : kEach / 8];       // a weight's first bf16 bits, and the next: together 2^-17 of it off
         float f[kWide ? kEach : 1];
     };
+    // (never 0 for a weight that isn't: an infinite value times either part is the same infinity. 2^-40 of it is far below what the sum shows)
+    static __device__ __forceinline__ float rest_of(float p) { return fmaf(p, 9.094947e-13f, p - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, p) & 0xffff0000u)); }
     static __device__ __forceinline__ Weights weights(const float (&p)[kEach])
     {
         Weights w{};
@@ -124,7 +126,11 @@ template <typename T, typename C, int D, bool EXACT> struct Shape {
             for (int e = 0; e < kEach; ++e) w.f[e] = p[e];
         } else {
 #pragma unroll
-            for (int e = 0; e < kEach / 2; ++e) w.v[e / 4][e % 4] = pack_bf16(p[2 * e], p[2 * e + 1]);
+            for (int e = 0; e < kEach / 2; ++e) {
+                const uint32_t a = __builtin_bit_cast(uint32_t, p[2 * e]), b = __builtin_bit_cast(uint32_t, p[2 * e + 1]);
+                w.v[e / 4][e % 4] = __builtin_amdgcn_perm(b, a, 0x07060302u);        // the upper halves
+                w.rest[e / 4][e % 4] = pack_bf16(rest_of(p[2 * e]), rest_of(p[2 * e + 1]));
+            }
         }
         return w;
     }
@@ -134,9 +140,15 @@ template <typename T, typename C, int D, bool EXACT> struct Shape {
 #pragma unroll
             for (int e = 0; e < kEach; ++e) o = mfma(kNarrow ? e4m3_of(v[e / 4], e % 4) : __builtin_bit_cast(f32x4, v)[e % 4], w.f[e], o);
         } else if constexpr (kNarrow) {
-            o = mfma(eight_bf16(v[0], v[1]), w.v[0], o);
-            o = mfma(eight_bf16(v[2], v[3]), w.v[1], o);
-        } else o = mfma(v, w.v[0], o);
+            const u32x4 a = eight_bf16(v[0], v[1]), b = eight_bf16(v[2], v[3]);
+            o = mfma(a, w.rest[0], o);
+            o = mfma(b, w.rest[1], o);
+            o = mfma(a, w.v[0], o);
+            o = mfma(b, w.v[1], o);
+        } else {
+            o = mfma(v, w.rest[0], o);
+            o = mfma(v, w.v[0], o);
+        }
         return o;
     }
 
