@@ -185,6 +185,36 @@ def test_captured_replayed_and_on_two_streams(ctx):
                 assert int(o.ids[r]) == want[0] and int(o.kept[r]) == want[2]
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("R,C", [(3, 131072), (300, 20000), (40, 3000)])
+def test_results_do_not_depend_on_timing(ctx, dtype, R, C):
+    rng = np.random.default_rng(R)
+    x, u = logits(rng, R, C, dtype), floats(rng.random(R))
+    p, k, m = floats(rng.choice([1.0, 0.95, 0.5], R)), whole(rng.choice([0, 0, 40, 700], R)), floats(rng.choice([0.0, 0.0, 0.01], R))
+    outs = [mt.alloc_samples(R, C) for _ in range(6)]
+    for o in outs:
+        mt.sample(ctx, x, u, o, top_p=p, top_k=k, min_p=m)
+    for o in outs[1:]:
+        assert torch.equal(o.ids, outs[0].ids) and torch.equal(o.kept, outs[0].kept) and torch.equal(o.logprobs, outs[0].logprobs)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_that_no_bin_suits(ctx, dtype):
+    """Masks of the type's lowest value, a few logits far in front, many equal ones in a narrow band, all settings."""
+    rng = np.random.default_rng(21)
+    C = 20000
+    x = 2.5 * rng.standard_normal((6, C), dtype=np.float32)
+    x[0, rng.random(C) < 0.95] = np.finfo(np.float32).min if dtype == "f32" else -3.38e38
+    x[1, :3] = 1e4
+    x[2] = 5.0 + 1e-4 * x[2]
+    x[3, rng.random(C) < 0.5] = 7.0
+    x[4] *= 1e-30
+    x[5] *= 1e6
+    t = torch.from_numpy(x).to(lc.DTYPES[dtype]).cuda()
+    for kw in (dict(), dict(top_p=[0.9] * 6), dict(top_k=[100] * 6), dict(top_k=[5000] * 6, top_p=[0.7] * 6), dict(min_p=[0.5] * 6, top_p=[0.6] * 6)):
+        check(ctx, t, rng.random(6), **kw)
+
+
 def test_many_rows(ctx):
     """The rows of a large batch, few of them looked at one by one."""
     rng = np.random.default_rng(13)
