@@ -512,7 +512,7 @@ typedef struct {
 /* Keys and values of the batch's rows into the pages of one layer: [heads][head_dim] elements a row, rounded once.  A row without a place (its sequence's
  * number out of range, its token beyond the table's width, its page's number out of range, more rows than tokens) is not written.
  * Errors: MT_EINVAL (null, a stride below heads x head_dim, layer out of range, rows other than n_seqs without first_row, max_new 0), MT_EUNSUPPORTED (rows neither MT_F32 nor MT_BF16, or
- * of another type than a cache that is not MT_KV8), MT_ESTATE (host-only context), MT_EDEVICE. */
+ * of another type than a cache that is not MT_KV8; more than 2^20 sequences in a batch, or 2^23 pairs of these and heads), MT_ESTATE (host-only context), MT_EDEVICE. */
 typedef struct {
     const void* k;              /* [rows][k_stride], dtype    */
     const void* v;              /* [rows][v_stride], dtype    */
@@ -529,8 +529,8 @@ mt_status mt_kv_write(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, c
  * number is out of range, or beyond the table's width, are not seen.  What stands in tokens that are not seen does not matter.
  * max_length: tokens of the longest sequence, which the work is cut by (0: the table's width); longer ones are served too, but slowly.
  * scratch: as in mt_score, of mt_attend_scratch_get's size for the call's sizes.
- * Errors: MT_EINVAL (null, q_heads no multiple of heads or 0, strides below q_heads x head_dim, layer out of range, scale not finite, scratch too small),
- * MT_EUNSUPPORTED (types as in mt_kv_write, more than 65535 query heads, 2^20 sequences in a batch or 2^23 pairs of these and heads), MT_ESTATE, MT_EDEVICE. */
+ * Errors: MT_EINVAL (null, q_heads no multiple of heads or 0, strides below q_heads x head_dim, layer out of range, scale not finite or beyond 1e38, scratch too small),
+ * MT_EUNSUPPORTED (as in mt_kv_write, and more than 65535 query heads), MT_ESTATE, MT_EDEVICE. */
 typedef struct {
     const void* q;              /* [rows][q_stride], dtype           */
     void* out;                  /* [rows][out_stride], dtype; may be q itself (same stride)  */

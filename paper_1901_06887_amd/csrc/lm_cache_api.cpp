@@ -131,7 +131,7 @@ mt_status mt_attend(mt_ctx* c, void* hip_stream, const mt_kv_cache* k, const mt_
     const uint64_t width = (uint64_t)a->q_heads * k->head_dim;
     if (b->rows && (!a->q || !a->out)) return ctx_fail(c, MT_EINVAL, "null rows");
     if (a->q_stride < width || a->out_stride < width) return ctx_fail(c, MT_EINVAL, "a stride is below the %llu elements of a row", (unsigned long long)width);
-    if (!std::isfinite(a->scale)) return ctx_fail(c, MT_EINVAL, "scale is not finite");
+    if (!std::isfinite(a->scale) || std::fabs(a->scale) > 1e38f) return ctx_fail(c, MT_EINVAL, "scale is not finite, or beyond 1e38");
     const uint64_t need = b->rows && b->n_seqs ? attend_scratch_bytes(*k, *b, a->q_heads, a->max_length) : 0;
     if (need && (!a->scratch || a->scratch_bytes < need || off16(a->scratch)))
         return ctx_fail(c, MT_EINVAL, "the call needs %llu bytes of scratch on a 16-byte boundary", (unsigned long long)need);

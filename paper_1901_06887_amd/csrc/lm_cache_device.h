@@ -24,7 +24,7 @@ __device__ __forceinline__ SeqRows seq_rows(const mt_kv_cache& c, const mt_kv_ba
     r.seq = there ? seq : -1;
     r.length = there ? max(c.lengths[seq], 0) : 0;
     r.first = max(f0, 0);
-    r.last = min(r.after, (int32_t)b.rows);
+    r.last = max(min(r.after, (int32_t)b.rows), r.first);         // (whatever first_row holds: last - first fits)
     return r;
 }
 

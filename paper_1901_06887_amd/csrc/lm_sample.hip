@@ -56,7 +56,7 @@ template <uint32_t WAVES> struct Lds {
         uint32_t count[kWaves][kBins];
         struct {
             uint64_t keys[kCap];
-            union { uint16_t notes[kNotes]; double weights[kThreads]; uint32_t counts[kBins]; };      // (weights of the first kThreads entries, once the notes have been read)
+            union { uint16_t notes[kNotes]; double weights[kThreads]; uint32_t counts[kBins > kThreads ? kBins : kThreads]; };      // (weights of the first kThreads entries, once the notes have been read)
         } list;
         uint64_t digits[256];
     };

@@ -144,6 +144,23 @@ def test_rows_of_nobody(ctx, dtype, kv8):
 
 
 @pytest.mark.parametrize("dtype,kv8", KINDS)
+@pytest.mark.parametrize("max_new", [1, 3, 40])
+def test_row_numbers_of_any_value(ctx, dtype, kv8, max_new):
+    """No row is touched that first_row does not put inside of the call's rows; nor are pages, by a write."""
+    c = Case(dtype, kv8, 1, 2, 64, 16, [40, 3])
+    low, high = -2 ** 31, 2 ** 31 - 1
+    for first in ([low, low], [high, high], [low, high], [high, low], [5, low], [low, -1], [3, 2], [7, 100], [-5, 0]):
+        out = torch.full_like(c.q, 7.0)
+        mt.attend(ctx, c.c, c.q, out, seqs=ints([0]), first_row=ints(first), max_new=max_new, scale=c.scale, scratch=mt.alloc_attend(ctx, c.c, c.q_heads, 1, max_new))
+        touched = [r for r in range(2) if first[0] <= r < first[1]]
+        assert torch.equal((out != 7.0).any(1).cpu(), torch.tensor([r in touched for r in range(2)]))
+        if not touched or first[1] > 1000:
+            before = [t.view(torch.uint8).clone() for t in (c.c.k, c.c.v)]
+            mt.kv_write(ctx, c.c, c.q[:, :64], c.q[:, :64], seqs=ints([0]), first_row=ints(first), max_new=max_new)
+            assert all(torch.equal(a, t.view(torch.uint8)) for a, t in zip(before, (c.c.k, c.c.v)))
+
+
+@pytest.mark.parametrize("dtype,kv8", KINDS)
 def test_pages_out_of_range_are_not_seen(ctx, dtype, kv8):
     """... and tokens beyond the table."""
     c = Case(dtype, kv8, 2, 4, 64, 16, [100, 64])

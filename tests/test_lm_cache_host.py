@@ -85,7 +85,7 @@ def test_rows_that_are_refused():
     refused(1, c.kv_write, 0, cache(), batch(), write_args(v=None))
     refused(1, c.kv_write, 0, cache(), batch(), write_args(v_stride=127))
     for kw, status in ((dict(q=None), 1), (dict(out=None), 1), (dict(out_stride=383), 1), (dict(q_heads=0), 1), (dict(q_heads=5), 1), (dict(q_heads=65536, q_stride=1 << 30, out_stride=1 << 30), 5),
-                       (dict(scale=float("inf")), 1), (dict(scale=float("nan")), 1)):
+                       (dict(scale=float("inf")), 1), (dict(scale=float("nan")), 1), (dict(scale=2e38), 1), (dict(scale=-1e38), 7)):
         refused(status, c.attend, 0, cache(), batch(), attend_args(**kw))
     lib = B.load_library()
     k, b, w, a = cache(), batch(), write_args(), attend_args()
