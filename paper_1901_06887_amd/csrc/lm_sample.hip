@@ -10,8 +10,12 @@
 //   top_p: weight per bin and wave in LDS in the first pass; a second one lists the bin that holds the bar. The weights of what is kept are then known for every wave's share
 //   neither: sums for every wave's share
 // The class is then looked for in the share that holds it, a few classes to a thread. Bins are laid by the lanes' largest first classes, so that neither a few very
-// large logits nor many very small ones (masks of the type's lowest value) spoil them: some 90 to a standard deviation of a bell-shaped row. A row for which a list does not suffice (thousands of classes in
+// large logits nor many very small ones (masks of the type's lowest value) spoil them. A row for which a list does not suffice (thousands of classes in
 // one bin, top_k of thousands) is settled digit by digit of the order's key: right, but sixteen and more passes.
+//
+// What bounds it, as measured: 1024 rows of 32768 fp32 classes with top_p take 88 us, 52 without (2.6 TB/s). The second is the 64-bit weights (some 45 vector instructions to a lane and class);
+// with top_p the weights' pass with its bins is about half, the pass that lists, from the caches and memory, a quarter, and bins, list and shares the rest. One row is a chain of
+// dependent steps: 15 us for 32768 classes with top_k, 37 for 64 masked bf16 rows of 65001 with top_k and top_p, where the list's pass is 10 and its order and sums the rest.
 #include "lm_cache_device.h"
 #include "lm_logits.h"
 
@@ -601,7 +605,8 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : MASK && sizeof(T
         }
         if (!settled && listed) {
             // in order: top_k by number, min_p by weight, top_p by sums
-            if (t.listed > kThreads && top_k <= kThreads && reached < top) cut_list(t, reached, top, top_k);
+            // (one row of 131072 bf16 classes, first 50: 25.4 us without the cut, 20.3 with it; 64 masked rows of 65001: 42.5, 37.0; lists of a few hundred are as fast either way)
+            if (t.listed > 400 && 2 * top_k <= t.listed && reached < top) cut_list(t, reached, top, top_k);
             const uint32_t n = t.listed, most_kept = min(n, top_k);
             put_in_order(t, n);
             weigh = Weigh(c, top);
@@ -886,7 +891,7 @@ template <typename T, uint32_t WAVES> hipError_t go(const SampleArgs& s, hipStre
 }
 // Waves of a workgroup: few where a row has little work for them, many where there are not two rows to a compute unit and much to do (us with 4 / 8 / 16 waves: 1024 rows of 1000 classes at top_p 0.9
 // 24.8 / 46.9 / 97, 512 of 8192 29.6 / 30.8 / 54.7, 1024 of 32768 88 / 91 / 148, all of them kept 57 / 52 / 78; 64 masked bf16 rows of 65001 with settings of their own 77 / 52 / 43, one of
-// 131072 at top_p 0.9 138 / 88 / 75, with top_k 50 41 / 21 / 25).
+// 131072 at top_p 0.9 138 / 88 / 75, with top_k 50 41 / 21 / 25; the last two with top_k before their lists were cut: 16 waves now 37 and 20).
 uint32_t waves_for(uint32_t rows, uint32_t classes)
 {
     if (classes <= 8192) return 4;

@@ -28,6 +28,7 @@
 //                   gap_kernel (global average pooling), head_kernel (softmax + argmax in
 //                   submission order), copy_kernel (the yardstick for byte counters)
 //   lm_norm.hip, lm_linear4.hip, lm_score.hip (helpers of their own: lm_device.h)
+//   lm_attend.hip, lm_kv_write.hip, lm_pages.hip, lm_sample.hip (lm_cache_device.h, lm_logits.h)
 //                   the operators behind language models' answers: residual and norm, layers of 4-bit weights,
 //                   what logits say about given classes
 //
