@@ -647,7 +647,11 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : MASK && sizeof(T
         if (settled) {
         } else if (top_p < 1.0f) {
             float lead;
-            const Bins bins = lay_bins(&lead);
+            Bins bins = lay_bins(&lead);
+            // They reach 2.5 standard deviations below the middle of a bell-shaped row, whose weights have their own middle sigma c ln 2 deviations higher: where less than what lies below (e^(-z^2/2) is
+            // several times that) is to be left out, bins of twice the width, down to 10. One row that is settled digit by digit instead takes 1024 rows of 32768 classes from 87 to 156 us.
+            const float z = 2.5f + (float)(c * 0.6931471805599453) * (128.0f / 1.4f) / bins.per;
+            if (exp2f(-0.72f * z * z) > 1.0f - top_p) bins.per *= 0.5f;
             if (least > 0) lead = top;
             double rest = 0;
             for (int round = 0; round < 2; ++round) {

@@ -215,6 +215,17 @@ def test_logits_that_no_bin_suits(ctx, dtype):
         check(ctx, t, rng.random(6), **kw)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("C", [700, 33000])
+def test_nearly_all_of_the_weight(ctx, dtype, C):
+    """Bars far below the middle of a row, at temperatures that make it flat or steep."""
+    rng = np.random.default_rng(C + 1)
+    top_p = [0.99, 0.9901, 0.999, 1 - 2.0 ** -14, 1 - 2.0 ** -19, 1 - 2.0 ** -24] * 3
+    x = logits(rng, 18, C, dtype)
+    check(ctx, x, rng.random(18), top_p=top_p, temperature=[0.6] * 6 + [1.0] * 6 + [6.0] * 6)
+    check(ctx, x, rng.random(18), top_p=top_p, min_p=[1e-6] * 18)
+
+
 def test_many_rows(ctx):
     """The rows of a large batch, few of them looked at one by one."""
     rng = np.random.default_rng(13)
