@@ -88,6 +88,10 @@ mt_status mt_debug_conv_launch(mt_ctx* ctx, uint32_t layer, uint32_t rows, const
  * Pure function of its arguments; needs no context and no device. */
 int mt_debug_linear4_shape(uint64_t tiles, uint32_t most_rows, uint32_t most_k, uint32_t compute_units, uint32_t x_dtype, uint32_t* outputs, uint32_t* rows);
 
+/* Test aid: the tokens *begin .. *stop - 1 of a sequence of `length` tokens, in a table of `reach` of them, that mt_kv_write walks over for its rows first .. last - 1 where it turns many rows' values
+ * around; row r is token length - (after - r).  last > first, after >= last, all below 2^31.  Both 0 where none has a place.  Pure function of its arguments; needs no context and no device. */
+void mt_debug_kv_write_places(uint32_t length, uint32_t first, uint32_t last, uint32_t after, uint32_t reach, uint32_t* begin, uint32_t* stop);
+
 /* Measurement aid: what a loop of nothing but bf16 matrix instructions sustains on the current
  * device.  Runs, on `stream`, a kernel in which every wavefront issues v_mfma_f32_32x32x16_bf16
  * on pseudo-random operands (eight independent accumulators, two wavefronts per SIMD, no memory

@@ -184,6 +184,8 @@ def load_library() -> ctypes.CDLL:
     L.mt_score.argtypes = [vp, vp, ctypes.POINTER(mt_score_args)]
     L.mt_debug_linear4_shape.argtypes = [ctypes.c_uint64, u32, u32, u32, u32, ctypes.POINTER(u32), ctypes.POINTER(u32)]
     L.mt_score_scratch_get.argtypes = [u32, u32, u32, u32, ctypes.POINTER(ctypes.c_uint64)]
+    L.mt_debug_kv_write_places.argtypes = [u32] * 5 + [ctypes.POINTER(u32)] * 2
+    L.mt_debug_kv_write_places.restype = None
     cache, batch, u64p = ctypes.POINTER(mt_kv_cache), ctypes.POINTER(mt_kv_batch), ctypes.POINTER(ctypes.c_uint64)
     L.mt_kv_write.argtypes = [vp, vp, cache, batch, ctypes.POINTER(mt_kv_write_args)]
     L.mt_attend.argtypes = [vp, vp, cache, batch, ctypes.POINTER(mt_attend_args)]
@@ -536,6 +538,13 @@ def debug_linear4_shape(groups: Sequence, compute_units: int, x_dtype: int) -> d
     lds = load_library().mt_debug_linear4_shape(sum(-(-r // 16) * -(-n // 16) for r, n, _ in there), max(r for r, _, _ in there), max(k for _, _, k in there), compute_units, x_dtype,
                                                 ctypes.byref(outputs), ctypes.byref(rows))
     return {"outputs": outputs.value, "rows": rows.value, "through_lds": bool(lds)}
+
+
+def debug_kv_write_places(length: int, first: int, last: int, after: int, reach: int) -> tuple:
+    """(begin, stop) of the tokens that mt_kv_write walks over for rows first .. last - 1 of a sequence, row r being token length - (after - r) of a table of `reach`."""
+    begin, stop = ctypes.c_uint32(), ctypes.c_uint32()
+    load_library().mt_debug_kv_write_places(length, first, last, after, reach, ctypes.byref(begin), ctypes.byref(stop))
+    return begin.value, stop.value
 
 
 def version() -> str:

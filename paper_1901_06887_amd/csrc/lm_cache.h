@@ -12,6 +12,15 @@ struct KvWriteArgs {
 };
 hipError_t launch_kv_write(const KvWriteArgs& a, hipStream_t s);
 
+// Places (tokens of a sequence) that rows first .. last - 1 of a call fill, row r being token length - (after - r) of a table of `reach` tokens: begin .. stop - 1.
+struct Places { int32_t begin, stop; };
+inline __host__ __device__ Places places_of_rows(int32_t length, int32_t first, int32_t last, int32_t after, int32_t reach)
+{
+    const int32_t from = length - (after - first), to = length - (after - last);
+    const Places p{from > 0 ? from : 0, to < reach ? to : reach};
+    return p.begin < p.stop ? p : Places{0, 0};
+}
+
 struct AttendArgs {
     mt_kv_cache c;
     mt_kv_batch b;

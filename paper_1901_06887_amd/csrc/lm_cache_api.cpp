@@ -2,6 +2,7 @@
 #include <cmath>
 
 #include "lm_cache.h"
+#include "../../include/mt_debug.h"
 
 using namespace mt;
 
@@ -109,6 +110,13 @@ mt_status mt_kv_write(mt_ctx* c, void* hip_stream, const mt_kv_cache* k, const m
     LM_TRY(c, hipSetDevice(v.device));
     LM_TRY(c, launch_kv_write(KvWriteArgs{*k, *b, *a}, (hipStream_t)hip_stream));
     return MT_OK;
+}
+
+void mt_debug_kv_write_places(uint32_t length, uint32_t first, uint32_t last, uint32_t after, uint32_t reach, uint32_t* begin, uint32_t* stop)
+{
+    const Places p = places_of_rows((int32_t)length, (int32_t)first, (int32_t)last, (int32_t)after, (int32_t)reach);
+    if (begin) *begin = (uint32_t)p.begin;
+    if (stop) *stop = (uint32_t)p.stop;
 }
 
 mt_status mt_attend_scratch_get(const mt_kv_cache* k, const mt_kv_batch* b, uint32_t q_heads, uint32_t max_length, uint64_t* bytes)

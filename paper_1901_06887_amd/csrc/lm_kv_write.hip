@@ -144,8 +144,9 @@ __global__ void __launch_bounds__(256) kv_write_many_kernel(KvWriteArgs w)
     C* tile = (C*)lds;                            // [kPlaces][row]
     const SeqRows s = seq_rows(c, w.b, entry);
     if (s.seq < 0 || s.last <= s.first) return;
-    const int32_t begin = max(s.upto(0) - 1, 0), stop = min(s.upto(s.last - 1 - s.first), (int32_t)(c.table_width * c.page_tokens));      // places of the rows
-    const int64_t row0 = (int64_t)s.first - (s.upto(0) - 1);                                                                          // (row of place 0)
+    const Places rows = places_of_rows(s.length, s.first, s.last, s.after, (int32_t)(c.table_width * c.page_tokens));
+    const int32_t begin = rows.begin, stop = rows.stop;
+    const int64_t row0 = (int64_t)s.first - (s.upto(0) - 1);      // (row of place 0)
     const T *k_rows = (const T*)w.a.k + h * D, *v_rows = (const T*)w.a.v + h * D;
     for (int32_t group = begin / (int32_t)kPlaces + (int32_t)blockIdx.y; group * (int32_t)kPlaces < stop; group += (int32_t)gridDim.y) {
         const int32_t base = group * (int32_t)kPlaces, lo = max(begin - base, 0), hi = min(stop - base, (int32_t)kPlaces);
