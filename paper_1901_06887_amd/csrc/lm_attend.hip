@@ -462,8 +462,10 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 || (sizeof(T) == 4 && siz
                     load_some(v, i, k);
 #pragma unroll
                     for (uint32_t e = 0; e < kAhead; ++e) {
-                        const float f = k + e < parts ? part_m[min(k + e, parts - 1)][cc] : 0;
-                        p = fmaf(v[e].a, f, p); r = fmaf(v[e].b, f, r);
+                        // (loads behind the last part have read it again: left out, not multiplied by 0, which an infinite sum would make NaN)
+                        const float f = part_m[min(k + e, parts - 1)][cc];
+                        p = k + e < parts ? fmaf(v[e].a, f, p) : p;
+                        r = k + e < parts ? fmaf(v[e].b, f, r) : r;
                     }
                 }
                 sums[0][cc][d] = p; sums[0][cc][d + 1] = r;
