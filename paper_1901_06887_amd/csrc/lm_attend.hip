@@ -463,9 +463,9 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 || (sizeof(T) == 4 && siz
 #pragma unroll
                     for (uint32_t e = 0; e < kAhead; ++e) {
                         // (loads behind the last part have read it again: left out, not multiplied by 0, which an infinite sum would make NaN)
-                        const float f = part_m[min(k + e, parts - 1)][cc];
-                        p = k + e < parts ? fmaf(v[e].a, f, p) : p;
-                        r = k + e < parts ? fmaf(v[e].b, f, r) : r;
+                        if (k + e >= parts) break;
+                        const float f = part_m[k + e][cc];
+                        p = fmaf(v[e].a, f, p); r = fmaf(v[e].b, f, r);
                     }
                 }
                 sums[0][cc][d] = p; sums[0][cc][d + 1] = r;
