@@ -525,6 +525,7 @@ mt_status mt_kv_write(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, c
  * q_heads is a multiple of the cache's heads; query heads h * q_heads / heads and on share head h of the cache.  lse = log sum_t e^(scale q.k_t), with
  * which results over several caches can be joined.  Products are exact for MT_BF16 and fp32 for MT_F32; sums and statistics are fp32; where rows are MT_BF16 weights
  * are off by 2^-17 of themselves on top; out is rounded once.
+ * A NaN among a row's products makes out and lse NaN; else one of +infinity (or beyond fp32's range) out NaN and lse +infinity.
  * A row that sees nothing (no tokens, its sequence's number out of range, or all its products -infinity) gets out 0 and lse -infinity.  Tokens in pages whose
  * number is out of range, or beyond the table's width, are not seen.  What stands in tokens that are not seen does not matter.
  * max_length: tokens of the longest sequence, which the work is cut by (0: the table's width); longer ones are served too, but slowly.

@@ -331,7 +331,8 @@ __global__ void __launch_bounds__(64 * kWaves, D > 128 || (sizeof(T) == 4 && siz
                 for (int e = 1; e < kEach; ++e) most = fmaxf(most, x[e]);
                 most = over_column(most, [](float p, float q) { return fmaxf(p, q); });
                 if (__ballot(most > m + kSlack)) {
-                    const float grown = most > m + kSlack ? most : m, f = factor(m, grown);
+                    // (never infinite: a product of +infinity has an infinite weight then, and so l, where infinity less infinity would say NaN)
+                    const float grown = most > m + kSlack ? fminf(most, -kLowest) : m, f = factor(m, grown);
                     m = grown;
                     l *= f;
 #pragma unroll
