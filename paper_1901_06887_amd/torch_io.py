@@ -158,13 +158,49 @@ class KVCache:
     [layers, pages, heads, page_tokens]; table int32 [seqs, width], lengths int32 [seqs], refs int32 [pages], work uint8."""
 
     def __init__(self, k, v, k_scales, v_scales, table, lengths, refs, work, dtype: int):
-        self.k, self.v, self.k_scales, self.v_scales, self.table, self.lengths, self.refs, self.work = k, v, k_scales, v_scales, table, lengths, refs, work
+        """A cache of the caller's own tensors, pages and layers as far apart as they like; refs and work may be None where no call on pages is made.  What does not fit is a ValueError."""
+        want = _wanted
+        kind = _KV_TYPES.get(dtype)
+        want(kind is not None, "of dtype MT_F32, MT_BF16 or MT_KV8")
+        want(isinstance(k, torch.Tensor) and k.dim() == 5 and k.dtype == kind, "k %s [layers, pages, heads, page_tokens, head_dim]" % kind)
         layers, pages, heads, page_tokens, head_dim = k.shape
+        page_stride, layer_stride = _blocks(k, "k", k.shape, (kind,), k.device)
+        want(_blocks(v, "v", (layers, pages, heads, head_dim, page_tokens), (kind,), k.device) == (page_stride, layer_stride), "v of k's strides between pages and layers")
+        scales = [(0, 0), (0, 0)]
+        if dtype == B.MT_KV8:
+            scales = [_blocks(t, name, (layers, pages, heads, page_tokens), (torch.float8_e8m0fnu, torch.uint8), k.device) for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales"))]
+        else:
+            want(k_scales is None and v_scales is None, "scales with MT_KV8 only")
+        want(scales[0] == scales[1], "v_scales of k_scales' strides")
+        want(_fits(table, 2, torch.int32, k.device) and (table.shape[1] <= 1 or table.stride(1) == 1) and (table.shape[0] <= 1 or table.stride(0) >= table.shape[1]), "table int32 [seqs, width], rows side by side")
+        want(_fits(lengths, 1, torch.int32, k.device) and lengths.numel() == table.shape[0] and lengths.is_contiguous(), "lengths int32 [%d], contiguous" % table.shape[0])
+        want(refs is None or _fits(refs, 1, torch.int32, k.device) and refs.numel() == pages and refs.is_contiguous(), "refs int32 [%d], contiguous" % pages)
+        want(work is None or _fits(work, 1, torch.uint8, k.device) and work.is_contiguous(), "work uint8, contiguous")
+        self.k, self.v, self.k_scales, self.v_scales, self.table, self.lengths, self.refs, self.work = k, v, k_scales, v_scales, table, lengths, refs, work
         p = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-        self.spec = B.mt_kv_cache(p(k), p(v), p(k_scales), p(v_scales), p(table), p(lengths), p(refs), p(work), k.stride(1), k.stride(0),
-                                  0 if k_scales is None else k_scales.stride(1), 0 if k_scales is None else k_scales.stride(0), table.stride(0), work.numel(),
-                                  dtype, layers, pages, heads, page_tokens, head_dim, table.shape[0], table.shape[1])
+        self.spec = B.mt_kv_cache(p(k), p(v), p(k_scales), p(v_scales), p(table), p(lengths), p(refs), p(work), page_stride, layer_stride, *scales[0],
+                                  max(table.stride(0), table.shape[1]), 0 if work is None else work.numel(), dtype, layers, pages, heads, page_tokens, head_dim, table.shape[0], table.shape[1])
         self._tensors = (k, v, k_scales, v_scales, table, lengths, refs)      # (the spec has their addresses)
+
+
+def _wanted(fits: bool, what: str) -> None:
+    if not fits:
+        raise ValueError("cache: %s wanted" % what)
+
+
+def _fits(t, dims: int, dtype, device) -> bool:
+    return isinstance(t, torch.Tensor) and t.dim() == dims and t.dtype == dtype and t.device == device
+
+
+def _blocks(t, name: str, shape, dtypes, device):
+    """Strides between pages and between layers of [layers, pages, ..], each page's block contiguous.  Where there is one alone: as if side by side."""
+    _wanted(isinstance(t, torch.Tensor) and t.shape == torch.Size(shape) and t.dtype in dtypes and t.device == device, "%s %s %s on %s" % (name, dtypes[0], list(shape), device))
+    block = 1
+    for size, stride in zip(reversed(t.shape[2:]), reversed(t.stride()[2:])):
+        _wanted(size <= 1 or stride == block, "%s with every page's elements side by side" % name)
+        block *= size
+    page = t.stride(1) if t.shape[1] > 1 else block
+    return page, t.stride(0) if t.shape[0] > 1 else page * t.shape[1]
 
 
 def alloc_kv(pages: int, page_tokens: int, heads: int, head_dim: int, seqs: int, width: int, dtype: int = B.MT_BF16, layers: int = 1, device="cuda:0") -> KVCache:

@@ -1,0 +1,68 @@
+"""What a cache of the caller's own tensors is refused for.  No GPU, no compute."""
+import pytest
+import torch
+
+import paper_1901_06887_amd as mt
+from paper_1901_06887_amd import binding as B
+
+L, P, H, T, D, S, W = 2, 4, 3, 16, 32, 5, 6
+NAMES = ("k", "v", "k_scales", "v_scales", "table", "lengths", "refs", "work")
+
+
+def parts(kind):
+    c = mt.alloc_kv(P, T, H, D, S, W, dtype=kind, layers=L, device="cpu")
+    return {n: getattr(c, n) for n in NAMES}
+
+
+def moved(t, *order):
+    """t with its dimensions in another order in memory."""
+    back = [order.index(i) for i in range(len(order))]
+    return t.view(torch.uint8 if t.element_size() == 1 else t.dtype).permute(order).contiguous().permute(back).view(t.dtype)
+
+
+@pytest.mark.parametrize("kind", [B.MT_F32, B.MT_BF16, B.MT_KV8])
+def test_tensors_that_do_not_fit(kind):
+    good = parts(kind)
+    k, v, table = good["k"], good["v"], good["table"]
+    bytes_of = lambda *shape: torch.zeros(shape, dtype=torch.uint8)  # noqa: E731
+    bad = [dict(k=moved(k, 0, 1, 3, 2, 4)), dict(v=moved(v, 0, 1, 2, 4, 3)), dict(k=moved(k, 0, 1, 2, 4, 3)), dict(v=moved(v, 0, 1, 3, 2, 4)),
+           dict(v=moved(v, 1, 0, 2, 3, 4)), dict(k=moved(k, 1, 0, 2, 3, 4)), dict(v=k), dict(k=v), dict(k=k[0]), dict(k=k[:, :3]), dict(v=v[:1]), dict(k=k[..., :16]), dict(k=k[:, :, :2]), dict(v=v[..., :8]),
+           dict(k=k.half() if kind == B.MT_F32 else k.float()), dict(v=v.half() if kind == B.MT_F32 else v.float()), dict(k=None), dict(v=None), dict(k=k.to("meta")), dict(table=table.to("meta")),
+           dict(table=table.long()), dict(table=table[0]), dict(table=table.t()), dict(table=table[:, ::2]), dict(table=table[:1].expand(S, W)), dict(table=None), dict(table=table.float()),
+           dict(lengths=torch.zeros(S - 1, dtype=torch.int32)), dict(lengths=torch.zeros(S, dtype=torch.int64)), dict(lengths=torch.zeros(2 * S, dtype=torch.int32)[::2]), dict(lengths=None),
+           dict(lengths=torch.zeros(S, 1, dtype=torch.int32)), dict(refs=torch.zeros(1, dtype=torch.int32)), dict(refs=torch.zeros(P, dtype=torch.int16)), dict(refs=torch.zeros(2 * P, dtype=torch.int32)[::2]),
+           dict(work=torch.zeros(1000, dtype=torch.float32)), dict(work=bytes_of(2000)[::2]), dict(work=bytes_of(10, 10)), dict(refs=torch.zeros(P + 1, dtype=torch.int32))]
+    if kind == B.MT_KV8:
+        ks = good["k_scales"]
+        bad += [dict(k_scales=None), dict(v_scales=None), dict(v_scales=moved(ks, 1, 0, 2, 3)), dict(k_scales=moved(ks, 0, 1, 3, 2)), dict(v_scales=moved(ks, 0, 1, 3, 2)), dict(k_scales=ks[:, :, :2]),
+                dict(v_scales=torch.zeros(L, P, H, T)), dict(k_scales=torch.zeros(L, P, H, T, dtype=torch.int8)), dict(k_scales=ks.to("meta"))]
+    else:
+        bad += [dict(k_scales=bytes_of(L, P, H, T)), dict(v_scales=bytes_of(L, P, H, T))]
+    for kw in bad:
+        with pytest.raises(ValueError, match="cache"):
+            mt.KVCache(**{**good, **kw}, dtype=kind)
+    for other in (B.MT_F32, B.MT_BF16, B.MT_KV8, B.MT_MX8, 17, None):
+        if other != kind:
+            with pytest.raises(ValueError, match="cache"):
+                mt.KVCache(**good, dtype=other)
+
+
+@pytest.mark.parametrize("kind", [B.MT_F32, B.MT_BF16, B.MT_KV8])
+def test_tensors_that_fit(kind):
+    """As alloc_kv makes them; layers inside of pages; pages apart from each other; a table inside of a wider one; tensors of one layer, page or sequence, whose strides say nothing; scales as bytes; no calls on pages."""
+    good = parts(kind)
+    inside = {n: moved(good[n], 1, 0, *range(2, good[n].dim())) for n in NAMES[:4] if good[n] is not None}
+    wide = {n: good[n][:, ::2] for n in NAMES[:4] if good[n] is not None}
+    spec = mt.KVCache(**{**good, **inside}, dtype=kind).spec
+    assert (spec.page_stride, spec.layer_stride) == (L * H * T * D, H * T * D) and (kind != B.MT_KV8 or (spec.scales_page_stride, spec.scales_layer_stride) == (L * H * T, H * T))
+    spec = mt.KVCache(**{**good, **wide, "refs": torch.zeros(2, dtype=torch.int32)}, dtype=kind).spec
+    assert (spec.n_pages, spec.page_stride, spec.layer_stride) == (2, 2 * H * T * D, P * H * T * D)
+    spec = mt.KVCache(**{**good, "table": torch.zeros(S, W + 3, dtype=torch.int32)[:, 1:W + 1]}, dtype=kind).spec
+    assert (spec.seqs, spec.table_width, spec.table_stride) == (S, W, W + 3)
+    one = {n: good[n][:1, :1].as_strided((1, 1, *good[n].shape[2:]), (7, 3, *good[n].stride()[2:])) for n in NAMES[:4] if good[n] is not None}
+    spec = mt.KVCache(**{**good, **one, "table": good["table"][:1, :1].as_strided((1, 1), (0, 9)), "lengths": torch.zeros(1, dtype=torch.int32), "refs": None, "work": None}, dtype=kind).spec
+    assert (spec.n_pages, spec.layers, spec.seqs, spec.table_width, spec.refs, spec.work, spec.work_bytes) == (1, 1, 1, 1, None, None, 0)
+    es = good["k"].element_size()
+    assert spec.page_stride * es % 16 == spec.layer_stride * es % 16 == spec.scales_page_stride % 16 == 0 and spec.table_stride >= 1
+    if kind == B.MT_KV8:
+        mt.KVCache(**{**good, "k_scales": good["k_scales"].view(torch.uint8), "v_scales": good["v_scales"].view(torch.uint8)}, dtype=kind)
