@@ -524,7 +524,8 @@ mt_status mt_kv_write(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, c
 /* out = sum_t p_t v_t with p = softmax(scale * q.k_t) over the tokens t that a row sees, head by head: those up to itself, of these the last `window` (0: all).
  * q_heads is a multiple of the cache's heads; query heads h * q_heads / heads and on share head h of the cache.  lse = log sum_t e^(scale q.k_t), with
  * which results over several caches can be joined.  Products are exact for MT_BF16 and fp32 for MT_F32; sums and statistics are fp32; where rows are MT_BF16 weights
- * are off by 2^-17 of themselves on top; out is rounded once.
+ * are off by up to 2^-16 of themselves on top; out is rounded once.  Sums are divided last and hold weights of up to 2^8 for every token: where those times the values (or these alone) leave fp32's range,
+ * out is infinite or NaN.
  * A NaN among a row's products makes out and lse NaN; else one of +infinity (or beyond fp32's range) out NaN and lse +infinity.
  * A row that sees nothing (no tokens, its sequence's number out of range, or all its products -infinity) gets out 0 and lse -infinity.  Tokens in pages whose
  * number is out of range, or beyond the table's width, are not seen.  What stands in tokens that are not seen does not matter.

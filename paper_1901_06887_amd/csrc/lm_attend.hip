@@ -117,7 +117,7 @@ template <typename T, typename C, int D, bool EXACT> struct Shape {
     // p: the weights as the second product takes them.
     static constexpr int kWeights = kWide ? kEach : kEach / 8;
     struct Weights {
-        u32x4 v[kWide ? 1 : kEach / 8], rest[kWide ? 1 : kEach / 8];       // a weight's first bf16 bits, and the next: together 2^-17 of it off
+        u32x4 v[kWide ? 1 : kEach / 8], rest[kWide ? 1 : kEach / 8];       // a weight's first bf16 bits, cut off, and the next, rounded: together up to 2^-16 of it off
         float f[kWide ? kEach : 1];
     };
     // (never 0 for a weight that isn't: an infinite value times either part is the same infinity. 2^-40 of it is far below what the sum shows)
