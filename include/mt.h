@@ -573,8 +573,8 @@ mt_status mt_kv_work_get(uint32_t n_pages, uint32_t seqs, uint64_t* bytes);
  *   weight (1 or more: all; the first always).
  * Drawn is the first kept class, in the order of class numbers, up to which the kept classes have more than uniform[i] of their weight (uniform in [0, 1): a class is drawn with
  * its share of the weight); with uniform of 1 or more the last one of any weight.  temperature 0 (or below 2^-126) keeps the first class alone.
- * Weights are off by 2^-39 of themselves and summed in 64 bits, in an order that depends on nothing but the inputs: a class whose border lies nearer than that to where top_p or the random number falls may
- * be taken for its neighbour.
+ * Weights and sums of them are off by up to 2^-39 of themselves, in 64 bits and in an order that depends on nothing but the inputs: where a border between classes lies nearer than that to where top_p or the
+ * random number falls, a class on its other side may be taken (several, where classes weigh less than that).
  *   ids[i]: the class; logprobs[i] = log of its share of the kept weight; kept[i]: classes kept.  Each may be NULL, not all.
  * A row without an allowed class: -1, -infinity, 0.  A row with a NaN or +infinity among its allowed classes or a setting that is NaN, or with a negative temperature: -1, NaN, -1.
  * scratch: as in mt_score, of mt_sample_scratch_get's size.

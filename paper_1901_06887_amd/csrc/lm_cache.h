@@ -67,7 +67,6 @@ hipError_t launch_kv_copy(const PagesArgs& a, hipStream_t s);
 
 struct SampleArgs {
     mt_sample_args a;
-    uint32_t bits;           // a weight of 1 is 2^bits
 };
 hipError_t prepare_sample();     // once per device, as prepare_pages
 uint64_t sample_scratch_bytes(uint32_t rows, uint32_t classes);

@@ -226,8 +226,6 @@ mt_status mt_sample(mt_ctx* c, void* hip_stream, const mt_sample_args* a)
     if (v.host_only) return ctx_fail(c, MT_ESTATE, "host-only context cannot run");
     if (a->rows == 0) return MT_OK;
     LM_TRY(c, hipSetDevice(v.device));
-    SampleArgs k{*a, 62};
-    while ((1u << (62 - k.bits)) < a->classes) --k.bits;
-    LM_TRY(c, launch_sample(k, (hipStream_t)hip_stream));
+    LM_TRY(c, launch_sample(SampleArgs{*a}, (hipStream_t)hip_stream));
     return MT_OK;
 }

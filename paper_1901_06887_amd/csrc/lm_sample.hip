@@ -783,23 +783,26 @@ __global__ void __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : MASK && sizeof(T
 
     if (!settled && next == kDigits) {
         weigh = Weigh(c, top);
-        const double unit = (double)(1ull << s.bits);
         const float least_x = least_logit(top, c, least, lane);
         uint64_t key = 1;
         if (top_k && top_k < x.n)
             key = max(key, reach(x.n, top_k, t, [&](uint32_t j, uint64_t* k) __attribute__((always_inline)) -> uint64_t { const float v = x.at(j); *k = order_key(v, j); return v > kNone; }));
         const uint64_t front = key;
-        const auto amount = [&](uint32_t j, uint64_t* k) __attribute__((always_inline)) -> uint64_t {
+        const auto weight = [&](uint32_t j, uint64_t* k) __attribute__((always_inline)) -> double {
             const float v = x.at(j);
             *k = order_key(v, j);
-            return v > kNone && *k >= front && v >= least_x ? (uint64_t)rint(weigh(v) * unit) : 0;
+            return v > kNone && *k >= front && v >= least_x ? weigh(v) : 0.0;
         };
         if (top_p < 1.0f) {
-            uint64_t sum = 0, k;
+            double sum = 0;
+            uint64_t k;
 #pragma nounroll
-            for (uint32_t j = tid; j < x.n; j += kThreads) sum += amount(j, &k);
-            sum = sum_all<uint64_t>(sum, t);
-            key = max(key, reach(x.n, (uint64_t)fmax(ceil((double)top_p * (double)sum), 1.0), t, amount));
+            for (uint32_t j = tid; j < x.n; j += kThreads) sum += weight(j, &k);
+            sum = sum_all<double>(sum, t);
+            // Whole numbers, so that digits' sums have no order; all of them together 2^61 to 2^62. Their roundings are 2^-42 of the sum for 2^20 classes, and no more than that of any front part that is the
+            // answer (whose classes are the largest). Multiples of a part of the *largest* weight instead lose small ones, which together may be what top_p is about.
+            const double unit = __builtin_bit_cast(double, (uint64_t)(2107 - (__builtin_bit_cast(uint64_t, sum) >> 52 & 0x7ff)) << 52);
+            key = max(key, reach(x.n, (uint64_t)fmax(ceil((double)top_p * sum * unit), 1.0), t, [&](uint32_t j, uint64_t* k) __attribute__((always_inline)) { return (uint64_t)rint(weight(j, k) * unit); }));
         }
         bar = key == 1 || key_logit(key) < least_x ? Bar{least_x, kNobody} : Bar{key_logit(key), (uint32_t)key_class(key)};
         next = kShares;
