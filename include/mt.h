@@ -558,7 +558,7 @@ mt_status mt_attend_scratch_get(const mt_kv_cache* cache, const mt_kv_batch* bat
  * mt_kv_compact: with n pages held, these are pages 0 .. n - 1 afterwards: the i-th held one from number n on moves into the i-th free one below (all layers), and the
  *   tables follow.  *live (DEVICE, or NULL) receives n.
  * mt_kv_copy: page from[i] is copied over page to[i] (all layers); tables and counts stay.  A pair out of range, or whose target an entry behind it names again, does nothing; a
- *   page that stands in both lists may be copied before or after it is overwritten.  n may be any number.
+ *   pair whose page from[i] is another pair's target leaves any mix of what that page held before and after in page to[i]: chains take a call for each link.  n may be any number.
  * Errors: MT_EINVAL (null list, refs or work, work too small, n over seqs), MT_ESTATE, MT_EDEVICE. */
 mt_status mt_kv_grow(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const int32_t* seqs, const int32_t* tokens, uint32_t n, int32_t* granted);
 mt_status mt_kv_fork(mt_ctx* ctx, void* hip_stream, const mt_kv_cache* cache, const int32_t* parents, const int32_t* children, uint32_t n, int32_t* granted);

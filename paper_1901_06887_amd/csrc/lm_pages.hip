@@ -292,7 +292,7 @@ __device__ void follow(const PagesArgs& p, const PageWork& work, uint32_t held)
 
 // Pages from and to of a list, whole: every workgroup takes pieces of kPiece bytes, 16 bytes a thread at a time.
 constexpr uint32_t kPiece = 16384;
-enum class Moves { kForked, kCompacted, kGiven };
+enum class Moves { kForked, kCompacted, kGiven, kClaimed };      // a list of the call's: every piece looks through what is behind its pair, or work.map says whose a page is
 struct Block { uint8_t* base; uint64_t page, layer; uint32_t bytes; };       // a page of one layer in one of the cache's four parts
 
 template <Moves WHAT>
@@ -300,7 +300,8 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(PagesArgs p)
 {
     const mt_kv_cache& c = p.c;
     const PageWork work = page_work(c);
-    const uint32_t n = WHAT == Moves::kGiven ? p.n : work.head->n;
+    constexpr bool given = WHAT == Moves::kGiven || WHAT == Moves::kClaimed;
+    const uint32_t n = given ? p.n : work.head->n;
     if constexpr (WHAT == Moves::kCompacted) follow(p, work, work.head->held);
     const uint32_t es = c.dtype == MT_F32 ? 4 : c.dtype == MT_BF16 ? 2 : 1;
     const uint32_t page = c.heads * c.page_tokens * c.head_dim * es, scales = c.dtype == MT_KV8 ? c.heads * c.page_tokens : 0;
@@ -309,13 +310,15 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(PagesArgs p)
     for (uint64_t i = blockIdx.x; i < all; i += gridDim.x) {
         const uint32_t pair = (uint32_t)(i / (c.layers * each)), rest = (uint32_t)(i % (c.layers * each)), layer = rest / each;
         uint32_t piece = rest % each;
-        const uint32_t from = (uint32_t)(WHAT == Moves::kGiven ? p.first[pair] : work.moves[2 * pair]), to = (uint32_t)(WHAT == Moves::kGiven ? p.second[pair] : work.moves[2 * pair + 1]);
+        const uint32_t from = (uint32_t)(given ? p.first[pair] : work.moves[2 * pair]), to = (uint32_t)(given ? p.second[pair] : work.moves[2 * pair + 1]);
         if (from >= c.n_pages || to >= c.n_pages || from == to) continue;
         if constexpr (WHAT == Moves::kGiven) {
             bool again = false;
             for (uint32_t j = pair + 1 + threadIdx.x; j < n; j += 256) again |= (uint32_t)p.second[j] == to;
             if (__syncthreads_or(again)) continue;
         }
+        if constexpr (WHAT == Moves::kClaimed)
+            if ((uint32_t)work.map[to] != pair + 1) continue;
         const bool second = piece >= pieces + scale_pieces;
         if (second) piece -= pieces + scale_pieces;
         const bool of_scales = piece >= pieces;
@@ -325,6 +328,21 @@ __global__ void __launch_bounds__(256) copy_pages_kernel(PagesArgs p)
         const uint8_t* src = base + from * stride + begin;
         uint8_t* dst = base + to * stride + begin;
         for (uint32_t at = threadIdx.x * 16; at < bytes; at += 256 * 16) *(u32x4*)(dst + at) = *(const u32x4*)(src + at);
+    }
+}
+
+// work.map: for every page the last pair, counted from 1, that names it as its target; 0 for none.
+__global__ void __launch_bounds__(256) unclaim_kernel(PagesArgs p)
+{
+    int32_t* map = page_work(p.c).map;
+    for (uint64_t i = blockIdx.x * 256 + threadIdx.x; i < p.c.n_pages; i += gridDim.x * 256) map[i] = 0;
+}
+__global__ void __launch_bounds__(256) claim_kernel(PagesArgs p)
+{
+    uint32_t* map = (uint32_t*)page_work(p.c).map;
+    for (uint64_t i = blockIdx.x * 256 + threadIdx.x; i < p.n; i += gridDim.x * 256) {
+        const uint32_t to = (uint32_t)p.second[i];
+        if (to < p.c.n_pages) atomicMax(&map[to], (uint32_t)i + 1);
     }
 }
 
@@ -357,6 +375,15 @@ hipError_t launch_kv_compact(const PagesArgs& p, hipStream_t s)
     const hipError_t e = launch(compact_kernel, dim3(1), kThreads, 0, s, p);
     return e != hipSuccess ? e : copy_pages<Moves::kCompacted>(p, p.c.n_pages, s);
 }
-hipError_t launch_kv_copy(const PagesArgs& p, hipStream_t s) { return copy_pages<Moves::kGiven>(p, p.n, s); }
+hipError_t launch_kv_copy(const PagesArgs& p, hipStream_t s)
+{
+    // Looking through the list is work that grows with its square (us looked through / looked up, pages of 4 KiB: 1 pair 5.7 / 13.9, 2048 8.9 / 13.2, 4096 18.5 / 16.6, 8192 42 / 24, 65536 1406 / 237; of 128 KiB:
+    // 1024 115 / 117, 4096 464 / 440).
+    if (p.n < 4096) return copy_pages<Moves::kGiven>(p, p.n, s);
+    const auto blocks = [](uint64_t n) { return dim3((uint32_t)std::min<uint64_t>((n + 255) / 256, 2048)); };
+    hipError_t e = launch(unclaim_kernel, blocks(p.c.n_pages), 256, 0, s, p);
+    if (e == hipSuccess) e = launch(claim_kernel, blocks(p.n), 256, 0, s, p);
+    return e != hipSuccess ? e : copy_pages<Moves::kClaimed>(p, p.n, s);
+}
 
 }  // namespace mt

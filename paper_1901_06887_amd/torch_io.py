@@ -272,7 +272,7 @@ def kv_compact(ctx: B.Context, cache: KVCache, live: Optional[torch.Tensor] = No
 
 
 def kv_copy(ctx: B.Context, cache: KVCache, from_pages: torch.Tensor, to_pages: torch.Tensor, stream: Optional[torch.cuda.Stream] = None) -> None:
-    """mt_kv_copy: pages of all layers copied over others."""
+    """mt_kv_copy: pages of all layers copied over others, none of them another pair's target (a chain takes a call for each link)."""
     st = (_answers or answers()).kv_copy(*_where(ctx, stream), cache.spec, cache._tensors, from_pages, to_pages)
     if st:
         ctx._check(st)
