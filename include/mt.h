@@ -577,8 +577,8 @@ mt_status mt_kv_work_get(uint32_t n_pages, uint32_t seqs, uint64_t* bytes);
  * random number falls, a class on its other side may be taken (several, where classes weigh less than that).
  *   ids[i]: the class; logprobs[i] = log of its share of the kept weight; kept[i]: classes kept.  Each may be NULL, not all.
  * A row without an allowed class: -1, -infinity, 0.  A row with a NaN or +infinity among its allowed classes or a setting that is NaN, or with a negative temperature: -1, NaN, -1.
- * scratch: as in mt_score, of mt_sample_scratch_get's size.
- * Errors: as mt_score; MT_EUNSUPPORTED for more than MT_SAMPLE_MAX_CLASSES classes too. */
+ * scratch: none is needed (mt_sample_scratch_get says 0, NULL will do); what is given stays as it is.
+ * Errors: as mt_score, but for the scratch; MT_EUNSUPPORTED for more than MT_SAMPLE_MAX_CLASSES classes too. */
 typedef struct {
     const void* logits;             /* [rows][row_stride], dtype                */
     const int32_t* n_classes;       /* [rows], or NULL; taken into 0 .. classes */

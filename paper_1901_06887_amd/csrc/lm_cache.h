@@ -69,7 +69,6 @@ struct SampleArgs {
     mt_sample_args a;
 };
 hipError_t prepare_sample();     // once per device, as prepare_pages
-uint64_t sample_scratch_bytes(uint32_t rows, uint32_t classes);
 hipError_t launch_sample(const SampleArgs& a, hipStream_t s);
 
 }  // namespace mt

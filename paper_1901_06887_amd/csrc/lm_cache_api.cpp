@@ -199,11 +199,11 @@ mt_status mt_kv_copy(mt_ctx* c, void* hip_stream, const mt_kv_cache* k, const in
     return call_pages(c, n, [&] { return launch_kv_copy(PagesArgs{*k, from, to, nullptr, n}, (hipStream_t)hip_stream); });
 }
 
-mt_status mt_sample_scratch_get(uint32_t rows, uint32_t classes, uint64_t* bytes)
+mt_status mt_sample_scratch_get(uint32_t, uint32_t classes, uint64_t* bytes)
 {
     if (!bytes || classes == 0) return MT_EINVAL;
     if (classes > MT_SAMPLE_MAX_CLASSES) return MT_EUNSUPPORTED;
-    *bytes = sample_scratch_bytes(rows, classes);
+    *bytes = 0;                  // (a row is one workgroup's, in LDS)
     return MT_OK;
 }
 
@@ -219,9 +219,6 @@ mt_status mt_sample(mt_ctx* c, void* hip_stream, const mt_sample_args* a)
         if (!a->logits || !a->uniform) return ctx_fail(c, MT_EINVAL, "null logits or random numbers");
         if (!a->ids && !a->logprobs && !a->kept) return ctx_fail(c, MT_EINVAL, "no output");
         if (a->row_stride < a->classes || (a->allowed && a->allowed_stride < (a->classes + 31) / 32)) return ctx_fail(c, MT_EINVAL, "a stride is below the %u classes", a->classes);
-        const uint64_t need = sample_scratch_bytes(a->rows, a->classes);
-        if (need && (!a->scratch || a->scratch_bytes < need || off16(a->scratch)))
-            return ctx_fail(c, MT_EINVAL, "the call needs %llu bytes of scratch on a 16-byte boundary", (unsigned long long)need);
     }
     if (v.host_only) return ctx_fail(c, MT_ESTATE, "host-only context cannot run");
     if (a->rows == 0) return MT_OK;

@@ -939,7 +939,6 @@ hipError_t prepare_sample()
     const hipError_t e = prepare<float, 16>();
     return e != hipSuccess ? e : prepare<__bf16, 16>();
 }
-uint64_t sample_scratch_bytes(uint32_t, uint32_t) { return 0; }
 
 hipError_t launch_sample(const SampleArgs& s, hipStream_t st) { return s.a.dtype == MT_BF16 ? all_rows<__bf16>(s, st) : all_rows<float>(s, st); }
 

@@ -460,10 +460,8 @@ PyObject* sample(PyObject*, PyObject* const* o, Py_ssize_t n)
         list_of(o[11], "ids", s.rows, kInt, w.device, &a.ids);
         list_of(o[12], "logprobs", s.rows, kF32, w.device, &a.logprobs);
         list_of(o[13], "kept", s.rows, kInt, w.device, &a.kept);
-        const at::Tensor& scratch = tensor(o[14], "scratch");
-        list_of(o[14], "scratch", scratch.numel(), at::kByte, w.device, &a.scratch);
-        a.scratch_bytes = scratch.numel();
-        return written(without_gil([&] { return sample_call(w.ctx, w.stream, &a); }), {o[11], o[12], o[13], o[14]});
+        if (o[14] != Py_None) list_of(o[14], "scratch", tensor(o[14], "scratch").numel(), at::kByte, w.device, &a.scratch);
+        return written(without_gil([&] { return sample_call(w.ctx, w.stream, &a); }), {o[11], o[12], o[13]});
     });
 }
 

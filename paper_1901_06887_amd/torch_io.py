@@ -284,11 +284,11 @@ class Samples:
     ids: Optional[torch.Tensor]              # int32 [R]
     logprobs: Optional[torch.Tensor]         # float32 [R]
     kept: Optional[torch.Tensor]             # int32 [R]
-    scratch: torch.Tensor                    # uint8
+    scratch: Optional[torch.Tensor] = None   # uint8; not used: a call needs none
 
 
 def alloc_samples(rows: int, classes: int, device="cuda:0") -> Samples:
-    """Outputs and scratch of mt_sample for so many rows and classes.  One call at a time may use them."""
+    """Outputs of mt_sample for so many rows and classes."""
     ints = lambda: torch.empty(rows, dtype=torch.int32, device=device)  # noqa: E731
     return Samples(ints(), torch.empty(rows, dtype=torch.float32, device=device), ints(), torch.zeros(B.sample_scratch(rows, classes), dtype=torch.uint8, device=device))
 

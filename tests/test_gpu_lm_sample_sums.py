@@ -93,3 +93,16 @@ def test_settings_together_settled_digit_by_digit(ctx, C):
         near = 2 * OFF * float(sums[-1] / w[r, kept - 1]) + 1
         assert abs(int(o.kept[r]) - kept) <= near and near < 20, (r, int(o.kept[r]), kept, near)
         assert int(o.ids[r]) == 5
+
+
+def test_calls_without_a_scratch(ctx):
+    x = torch.randn(3, 70000, device="cuda")
+    outs = [mt.alloc_samples(3, 70000) for _ in range(3)]
+    outs[1].scratch, outs[2].scratch = None, torch.full((5,), 7, dtype=torch.uint8, device="cuda")
+    for o in outs:
+        mt.sample(ctx, x, floats([0.3, 0.6, 0.9]), o, top_p=floats([0.9] * 3))
+    assert all(torch.equal(o.ids, outs[0].ids) and torch.equal(o.kept, outs[0].kept) for o in outs) and torch.all(outs[2].scratch == 7)
+    for bad in (torch.zeros(4, device="cuda"), torch.zeros(4, dtype=torch.uint8), "x"):
+        outs[1].scratch = bad
+        with pytest.raises(ValueError):
+            mt.sample(ctx, x, floats([0.3] * 3), outs[1])

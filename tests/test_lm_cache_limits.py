@@ -2,6 +2,8 @@
 import itertools
 
 import paper_1901_06887_amd as mt
+from test_lm_cache_host import sample_args
+from test_lm_host import host_ctx, refused
 
 HIGH = 2 ** 31 - 1
 
@@ -14,3 +16,12 @@ def test_places_of_rows_of_any_length():
                                                                  [(0, 1, 1), (0, 16, 16), (5, 21, 21), (0, 16, 100), (3, 40, HIGH), (HIGH - 20, HIGH - 2, HIGH), (0, HIGH, HIGH)]):
         begin, stop = max(length - (after - first), 0), min(length - (after - last), reach)
         assert mt.debug_kv_write_places(length, first, last, after, reach) == ((begin, stop) if begin < stop else (0, 0)), (length, reach, first, last, after)
+
+
+def test_sampling_needs_no_scratch():
+    c = host_ctx()
+    for rows, classes in ((1, 1), (1, 1 << 20), (100000, 65001)):
+        assert mt.sample_scratch(rows, classes) == 0
+    for kw in (dict(scratch=None, scratch_bytes=0), dict(scratch=72, scratch_bytes=1)):
+        refused(7, c.sample, 0, sample_args(**kw))
+    c.close()
