@@ -1,8 +1,8 @@
 // mt_kv_write: new tokens' keys and values into their pages.
 //
 // A token's keys lie side by side, its values page_tokens apart; in 8 bits a token and head share the power of two that the largest magnitude takes. A few tokens of a sequence: a wave to a token and head,
-// its values scattered element by element (256 sequences of one token, eight heads of 128, in 8 bits: 5 us, a chain of three trips to memory). Many: a workgroup to a head and 64 places side by
-// side, values turned around in LDS and written 16 bytes of a feature at a time (eight prompts of 1500 to 4096 tokens, eight heads of 128 bf16 elements: 61 us, 3.9 TB/s; pairs of elements to a lane, half of the
+// its values scattered element by element (256 sequences of one token, eight heads of 128, in 8 bits: 6.3 us, a chain of three trips to memory). Many: a workgroup to a head and 64 places side by
+// side, values turned around in LDS and written 16 bytes of a feature at a time (eight prompts of 1500 to 4096 tokens, eight heads of 128 bf16 elements: 58.6 us, 4.1 TB/s; into 8 bits 56, 3.2; pairs of elements to a lane, half of the
 // loads on their way: 107).
 #include <type_traits>
 
