@@ -162,10 +162,11 @@ class KVCache:
         want = _wanted
         kind = _KV_TYPES.get(dtype)
         want(kind is not None, "of dtype MT_F32, MT_BF16 or MT_KV8")
-        want(isinstance(k, torch.Tensor) and k.dim() == 5 and k.dtype == kind, "k %s [layers, pages, heads, page_tokens, head_dim]" % kind)
+        kinds = (kind, torch.uint8) if dtype == B.MT_KV8 else (kind,)          # (8-bit values also as their bytes, scales too)
+        want(isinstance(k, torch.Tensor) and k.dim() == 5 and k.dtype in kinds, "k %s [layers, pages, heads, page_tokens, head_dim]" % kind)
         layers, pages, heads, page_tokens, head_dim = k.shape
-        page_stride, layer_stride = _blocks(k, "k", k.shape, (kind,), k.device)
-        want(_blocks(v, "v", (layers, pages, heads, head_dim, page_tokens), (kind,), k.device) == (page_stride, layer_stride), "v of k's strides between pages and layers")
+        page_stride, layer_stride = _blocks(k, "k", k.shape, kinds, k.device)
+        want(_blocks(v, "v", (layers, pages, heads, head_dim, page_tokens), kinds, k.device) == (page_stride, layer_stride), "v of k's strides between pages and layers")
         scales = [(0, 0), (0, 0)]
         if dtype == B.MT_KV8:
             scales = [_blocks(t, name, (layers, pages, heads, page_tokens), (torch.float8_e8m0fnu, torch.uint8), k.device) for t, name in ((k_scales, "k_scales"), (v_scales, "v_scales"))]

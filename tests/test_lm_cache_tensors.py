@@ -65,4 +65,4 @@ def test_tensors_that_fit(kind):
     es = good["k"].element_size()
     assert spec.page_stride * es % 16 == spec.layer_stride * es % 16 == spec.scales_page_stride % 16 == 0 and spec.table_stride >= 1
     if kind == B.MT_KV8:
-        mt.KVCache(**{**good, "k_scales": good["k_scales"].view(torch.uint8), "v_scales": good["v_scales"].view(torch.uint8)}, dtype=kind)
+        mt.KVCache(**{**good, **{n: good[n].view(torch.uint8) for n in NAMES[:4]}}, dtype=kind)
